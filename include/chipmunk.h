@@ -36,7 +36,7 @@ extern "C" {
 #define CHIPMUNK_ERR_NULL         -1  /* a required pointer is NULL */
 #define CHIPMUNK_ERR_SHAPE        -2  /* a size is out of range (<= 0, k > C, k_stride < k, ...) */
 #define CHIPMUNK_ERR_ALIGN        -3  /* a pointer or leading dimension breaks the alignment rule */
-#define CHIPMUNK_ERR_UNSUPPORTED  -4  /* E not in {64,128}, c not in {128,192}, D % 128 or F % 64 != 0, unknown act */
+#define CHIPMUNK_ERR_UNSUPPORTED  -4  /* E not in {64,128}, c not in {128,192}, D % 128 or F % 64 != 0, unknown act or dtype, ... */
 #define CHIPMUNK_ERR_WORKSPACE    -5  /* workspace missing or too small */
 #define CHIPMUNK_ERR_LAUNCH       -6  /* the HIP runtime refused a launch */
 
@@ -270,6 +270,64 @@ int32_t chipmunk_mlp_dense(const uint16_t* x, const uint16_t* w1, const uint16_t
                            const uint16_t* w2, const uint16_t* b2, uint16_t* out,
                            uint16_t* a_cache, int64_t a_ld,
                            int B, int N, int D, int F, int c, int act, void* stream);
+
+/* ---- The attention half of a block around the kernels above, and a text encoder's: projections, rotary positions, and
+ * attention over packed sequences.  Elements are bf16 or fp16 (dtype), raw 16-bit values as above; strides are in elements,
+ * multiples of 8, of rows that do not overlap; positions and lengths are on the device, and no call reads them on the host. ---- */
+
+#define CHIPMUNK_DTYPE_BF16  0
+#define CHIPMUNK_DTYPE_FP16  1
+
+#define CHIPMUNK_ACT_NONE  2   /* chipmunk_linear only, which takes CHIPMUNK_ACT_GELU_* as well */
+#define CHIPMUNK_ACT_SILU  3
+
+/* Linear layer with what follows it in one call:
+ *   out[n,f] = act(<x[n], w[f]> + bias[f]) + residual[n,f],
+ * products accumulated in fp32, everything after them in fp32, rounded once.
+ * x: [N,D], row stride ldx; w: [F,D] dense; bias: [F] or NULL; residual: [N,F],
+ * row stride ldr, or NULL; out: [N,F], row stride ldo.  out may be residual
+ * (same pointer and stride) and overlaps nothing else.  The values between a
+ * row's end and the next row are neither read nor written.  D and F multiples
+ * of 8, D < 2^20, row strides < 2^22.  silu(y) = y / (1 + exp(-y)). */
+int32_t chipmunk_linear(const uint16_t* x, int64_t ldx, const uint16_t* w, const uint16_t* bias,
+                        const uint16_t* residual, int64_t ldr, uint16_t* out, int64_t ldo,
+                        int N, int D, int F, int act, int dtype, void* stream);
+
+/* Rotary positions with several axes (time, height, width).  Of a head's E elements the first 2 P, P = pairs_t + pairs_h +
+ * pairs_w, are P pairs: elements 2 j and 2 j + 1, or with `halves` j and j + P.  Pair j belongs to axis 0 (the first pairs_t), 1
+ * (the next pairs_h) or 2 and is turned by angle = pos[t][axis] * freqs[j]:
+ *   (a, b) -> (a cos(angle) - b sin(angle), a sin(angle) + b cos(angle));
+ * `inverse` turns by -angle, which is also the gradient of the turn.  Elements from 2 P on are copied.
+ * x, out: element e of head h of token t at t * token stride + h * head stride + e, so rows of heads ([tokens, heads, E], also
+ * inside a projection's result) and heads of rows ([heads, tokens, E]) alike, and from one to the other.  out may be x (same
+ * pointer and strides) and overlaps nothing else.  pos: [tokens,3] int32; freqs: [P] fp64, radians per position: angles are
+ * formed in fp64, sines and products in fp32, rounded once.  E a multiple of 8 up to 512, P of 4 (halves: 8), heads <= 65536. */
+int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* pos, const double* freqs,
+                      uint16_t* out, int64_t out_token_stride, int64_t out_head_stride, int tokens, int heads, int E,
+                      int pairs_t, int pairs_h, int pairs_w, int halves, int inverse, int dtype, void* stream);
+
+/* Attention over S packed sequences of different lengths, heads grouped: query head h reads key head h / (Hq / Hk).
+ * Sequence s has the queries cu_q[s] .. cu_q[s+1] - 1 of q (n_q of them) and the keys cu_k[s] .. cu_k[s+1] - 1 of k and v or,
+ * with k_len, the first k_len[s] from cu_k[s] on (n_k of them; caches with room behind).  Its query i sees its key j if not
+ * `causal`, or if j <= i + n_k - n_q: the last query sees every key.
+ *   out[i,h] = softmax_j(softmax_scale * <q[i,h], k[j]>) v[j]     over the keys that are seen; none: zero.
+ * Scores, softmax and sums are fp32; a probability is rounded to the element type where it meets v, and so in its sum.  Keys that
+ * a query does not see have no influence on it, whatever k and v hold there.
+ * q, k, v, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E (a head stride
+ * of one head alone does not count).  Tq, Tk: rows of q (and out) and of k and v.  Rows of out that belong to no sequence are
+ * left as they were.  max_q, max_k: no sequence has more queries, keys; sequences that do are cut there, which gives wrong
+ * results.  cu_q, cu_k: [S+1] int32 ascending; with k_len, cu_k[S] is not read.  Entries are clamped so that bad ones give wrong
+ * results, not accesses outside the tensors.
+ * E in {64,128}; token strides < 2^24.  ws: chipmunk_attn_packed_workspace_bytes() (0: ws may be NULL; also 0 on bad
+ * arguments), contents undefined afterwards, not to be shared by calls that may overlap. */
+size_t chipmunk_attn_packed_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k);
+int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,
+                             const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride,
+                             const uint16_t* v, int64_t v_token_stride, int64_t v_head_stride,
+                             uint16_t* out, int64_t out_token_stride, int64_t out_head_stride,
+                             const int32_t* cu_q, const int32_t* cu_k, const int32_t* k_len,
+                             int S, int Tq, int Tk, int Hq, int Hk, int E, int max_q, int max_k, int causal,
+                             float softmax_scale, int dtype, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

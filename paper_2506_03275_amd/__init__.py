@@ -25,6 +25,8 @@ _c_size = ctypes.c_size_t
 
 ACT_GELU_ERF = 0
 ACT_GELU_TANH = 1
+ACT_NONE = 2   # linear only, like ACT_SILU
+ACT_SILU = 3
 
 _SIGNATURES = {
     "chipmunk_voxel_reorder": ([_c_ptr] * 4 + [_c_int] * 11 + [_c_ptr], ctypes.c_int32),
@@ -51,6 +53,10 @@ _SIGNATURES = {
     "chipmunk_mlp_sparse_delta_overlapped": ([_c_ptr] * 7 + [_c_i64, _c_ptr] + [_c_int] * 7 + [_c_ptr, _c_size, _c_ptr],
                                              ctypes.c_int32),
     "chipmunk_mlp_dense": ([_c_ptr] * 7 + [_c_i64] + [_c_int] * 6 + [_c_ptr], ctypes.c_int32),
+    "chipmunk_linear": ([_c_ptr, _c_i64, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_ptr, _c_i64] + [_c_int] * 5 + [_c_ptr], ctypes.c_int32),
+    "chipmunk_rope": ([_c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_i64] + [_c_int] * 9 + [_c_ptr], ctypes.c_int32),
+    "chipmunk_attn_packed_workspace_bytes": ([_c_int] * 6, _c_size),
+    "chipmunk_attn_packed": ([_c_ptr, _c_i64, _c_i64] * 4 + [_c_ptr] * 3 + [_c_int] * 9 + [_c_f32, _c_int, _c_ptr, _c_size, _c_ptr], ctypes.c_int32),
     "chipmunk_status_string": ([ctypes.c_int32], ctypes.c_char_p),
 }
 
@@ -368,3 +374,102 @@ def mlp_dense(x, w1, b1, w2, b2, out, a_cache, c, act):
                                      _ptr(b2, bf, "b2"), _ptr(out, bf, "out"), _ptr(a_cache, bf, "a_cache"),
                                      a_cache.shape[-1], B, N, D, F, c, int(act), _stream()),
            "chipmunk_mlp_dense")
+
+
+# ---- projections, rotary positions, attention over packed sequences ------------------------------------------------------
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _strided(t, dtype, name, dims):
+    """Pointer of a tensor of so many dimensions whose last one is dense; None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError(f"{name}: expected a torch tensor of {dtype}")
+    if t.dim() != dims:
+        raise ValueError(f"{name}: must have {dims} dimensions")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: must live on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: must live on the current device")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: rows must be dense")
+    return t.data_ptr()
+
+
+def _element(t, name):
+    """The element type that all tensors of a call share, and its number."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES:
+        raise TypeError(f"{name}: expected a torch tensor of bfloat16 or float16")
+    return t.dtype, _DTYPES[t.dtype]
+
+
+def linear(x, w, bias, residual, out, act=ACT_NONE):
+    """out = act(x w^T + bias) + residual.  x: [N, D], residual (or None), out: [N, F], rows dense, any row stride; w: [F, D], bias:
+    [F] or None, contiguous; all bf16 or all fp16.  out may be residual."""
+    dtype, number = _element(x, "x")
+    px, pr, po = _strided(x, dtype, "x", 2), _strided(residual, dtype, "residual", 2), _strided(out, dtype, "out", 2)
+    pw, pb = _strided(w, dtype, "w", 2), _strided(bias, dtype, "bias", 1)
+    (N, D), F = x.shape, w.shape[0]
+    if not w.is_contiguous() or w.shape[1] != D:
+        raise ValueError("w: must be contiguous, with rows as long as x's")
+    if tuple(out.shape) != (N, F) or (residual is not None and residual.shape != out.shape) or (bias is not None and bias.shape[0] != F):
+        raise ValueError("out and residual must be [rows of x, rows of w], bias [rows of w]")
+    _check(load().chipmunk_linear(px, _row_stride(x), pw, pb, pr, 0 if residual is None else _row_stride(residual), po, _row_stride(out), N, D, F,
+                                  int(act), number, _stream()), "chipmunk_linear")
+
+
+def _row_stride(t):
+    """A single row's stride means nothing."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
+
+
+def rope_frequencies(axes, theta=10000.0, device="cuda"):
+    """The usual frequencies of rope: theta ** (-i / pairs) for pair i of an axis of so many pairs, fp64 [sum(axes)]."""
+    return torch.cat([theta ** (-torch.arange(n, dtype=torch.float64, device=device) / max(n, 1)) for n in axes])
+
+
+def rope(x, pos, freqs, out, axes, halves=False, inverse=False):
+    """Rotary positions.  x, out: [tokens, heads, E] bf16 or fp16, any strides of tokens and heads (x.transpose(0, 1) of heads of
+    rows); out may be x.  pos: int32 [tokens, 3]; freqs: fp64 [pairs]; axes: pairs of the three axes; halves: pair j is elements j
+    and j + pairs, else 2 j and 2 j + 1; inverse: by the opposite angle, the gradient of the turn."""
+    dtype, number = _element(x, "x")
+    px, po = _strided(x, dtype, "x", 3), _strided(out, dtype, "out", 3)
+    pp, pf = _strided(pos, torch.int32, "pos", 2), _strided(freqs, torch.float64, "freqs", 1)
+    tokens, heads, E = x.shape
+    t, h, w = axes
+    if out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    if tuple(pos.shape) != (tokens, 3) or not pos.is_contiguous() or freqs.shape[0] != t + h + w:
+        raise ValueError("pos must be contiguous [tokens, 3], freqs [pairs of all axes]")
+    _check(load().chipmunk_rope(px, x.stride(0), x.stride(1), pp, pf, po, out.stride(0), out.stride(1), tokens, heads, E, t, h, w,
+                                int(bool(halves)), int(bool(inverse)), number, _stream()), "chipmunk_rope")
+
+
+def attn_packed_workspace_bytes(S, Hq, Hk, E, max_q, max_k):
+    return int(load().chipmunk_attn_packed_workspace_bytes(S, Hq, Hk, E, max_q, max_k))
+
+
+def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k_len=None, ws=None):
+    """Attention over packed sequences.  q, out: [Tq, Hq, E], k, v: [Tk, Hk, E], bf16 or fp16, any strides of rows and heads; cu_q,
+    cu_k: int32 [S + 1], where the sequences start; k_len: int32 [S] or None, keys in use from there on; max_q, max_k: no
+    sequence has more queries, keys; ws: uint8 workspace of attn_packed_workspace_bytes (none needed where that is 0)."""
+    dtype, number = _element(q, "q")
+    i32 = torch.int32
+    pq, pk, pv, po = (_strided(t, dtype, name, 3) for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out")))
+    pcq, pck, pkl = _strided(cu_q, i32, "cu_q", 1), _strided(cu_k, i32, "cu_k", 1), _strided(k_len, i32, "k_len", 1)
+    pws = _strided(ws, torch.uint8, "ws", 1)
+    (Tq, Hq, E), (Tk, Hk, _), S = q.shape, k.shape, cu_q.shape[0] - 1
+    if out.shape != q.shape or k.shape != v.shape or k.shape[2] != E:
+        raise ValueError("out must have the shape of q, v that of k, and all the same E")
+    if cu_k.shape[0] != S + 1 or (k_len is not None and k_len.shape[0] != S):
+        raise ValueError("cu_q and cu_k must be [sequences + 1], k_len [sequences]")
+    strides = [s for t in (q, k, v, out) for s in (_row_stride3(t), t.stride(1))]
+    _check(load().chipmunk_attn_packed(pq, strides[0], strides[1], pk, strides[2], strides[3], pv, strides[4], strides[5], po, strides[6], strides[7],
+                                       pcq, pck, pkl, S, Tq, Tk, Hq, Hk, E, max_q, max_k, int(bool(causal)), float(softmax_scale), number,
+                                       pws, 0 if ws is None else ws.numel(), _stream()), "chipmunk_attn_packed")
+
+
+def _row_stride3(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[2]

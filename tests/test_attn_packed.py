@@ -1,0 +1,337 @@
+"""Attention over packed sequences against its definition in 64 bits, and what it refuses.
+
+Tolerance.  With w_j the weights of a row and A = sum_j w_j |v_j|: a weight is rounded to the element type, by half a step, eps / 2
+of its value at most, in the products with v and in their sum alike, so the row moves by eps / 2 (A + |out|); the result is rounded
+once, eps / 2 |out|.  A score is a sum of E products in 32 bits that pass E / 8 + 8 roundings at most, and is read off by an
+exponential as far from one: together d = 2^-24 ((E / 8 + 10) sum |q k| scale + 2 |score| + 8), which moves the row by 2 d A.  In fp16
+a weight below 2^-14 of the largest is rounded in steps of 2^-24, so n_k of them add 2^-25 n_k max |v| at most."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+DEV = "cuda"
+TYPES = [torch.bfloat16, torch.float16]
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def cm():
+    import paper_2506_03275_amd as cm
+    cm.load()
+    return cm
+
+
+def _starts(lengths):
+    return [sum(lengths[:i]) for i in range(len(lengths) + 1)]
+
+
+def reference(q, k, v, causal, scale):
+    """One sequence: q [n_q, Hq, E], k, v [n_k, Hk, E] -> the result in 64 bits and how far the kernel's may be from it."""
+    (nq, Hq, E), (nk, Hk, _) = q.shape, k.shape
+    info = torch.finfo(q.dtype)
+    out, off = torch.zeros(nq, Hq, E, dtype=torch.float64, device=q.device), torch.zeros(nq, Hq, E, dtype=torch.float64, device=q.device)
+    if nk == 0:
+        return out, off
+    seen = torch.arange(nk, device=q.device) <= (torch.arange(nq, device=q.device)[:, None] + (nk - nq if causal else nk))
+    for h in range(Hq):
+        qh, kh, vh = q[:, h].double(), k[:, h // (Hq // Hk)].double(), v[:, h // (Hq // Hk)].double()
+        s = (qh @ kh.t() * scale).masked_fill(~seen, -math.inf)
+        m = s.amax(1, keepdim=True).clamp(min=-1e300)
+        p = torch.exp(s - m)
+        p = p / p.sum(1, keepdim=True).clamp(min=1e-300)
+        out[:, h] = p @ vh
+        A = p @ vh.abs()
+        d = 2.0 ** -24 * ((E / 8 + 10) * (qh.abs() @ kh.abs().t()) * scale + 2 * s.abs() + 8).masked_fill(~seen, 0).amax(1, keepdim=True)
+        off[:, h] = info.eps / 2 * (A + 2 * out[:, h].abs()) * 1.02 + 2 * d * A + info.tiny * info.eps
+        if q.dtype == torch.float16:
+            off[:, h] += 2.0 ** -25 * nk * vh.abs().amax()
+    return out, off
+
+
+def _inputs(nq, nk, Hq, Hk, E, dtype, seed, slot=0, scale=1.0, packed=False):
+    """q, k, v of the sequences one behind the other, k and v in slots of so many rows; what belongs to no sequence is NaN."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    at_q, at_k = _starts(nq), [i * slot for i in range(len(nk) + 1)] if slot else _starts(nk)
+    r = lambda n, H: (torch.randn((max(n, 1), H, E), generator=g, device=DEV) * scale).to(dtype)   # noqa: E731
+    if packed:   # side by side, as a projection leaves them
+        rows = r(at_q[-1], Hq + 2 * Hk)
+        q, k, v = rows[:, :Hq], rows[:, Hq:Hq + Hk], rows[:, Hq + Hk:]
+    else:
+        q, k, v = r(at_q[-1], Hq), r(at_k[-1], Hk), r(at_k[-1], Hk)
+    if slot:
+        for s, n in enumerate(nk):
+            k[at_k[s] + n:at_k[s + 1]] = math.nan
+            v[at_k[s] + n:at_k[s + 1]] = math.nan
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)   # noqa: E731
+    return q, k, v, i32(at_q), i32(at_k), i32(nk) if slot else None
+
+
+def _run(cm, q, k, v, cu_q, cu_k, k_len, nq, nk, causal, scale, out=None, max_q=None, max_k=None):
+    S, (_, Hq, E), Hk = len(nq), q.shape, k.shape[1]
+    max_q, max_k = max_q or max(max(nq), 1), max_k or max(max(nk), 1)
+    ws = torch.full((max(16, cm.attn_packed_workspace_bytes(S, Hq, Hk, E, max_q, max_k)),), 255, dtype=torch.uint8, device=DEV)
+    if out is None:
+        out = torch.full((q.shape[0], Hq, E), math.nan, dtype=q.dtype, device=DEV)
+    cm.attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, scale, k_len=k_len, ws=ws)
+    return out
+
+
+def _check(cm, nq, nk, Hq, Hk, E, dtype, causal, seed=0, slot=0, scale=None, size=1.0, packed=False, **more):
+    scale = scale or 1 / math.sqrt(E)
+    q, k, v, cu_q, cu_k, k_len = _inputs(nq, nk, Hq, Hk, E, dtype, seed, slot, size, packed)
+    out = _run(cm, q, k, v, cu_q, cu_k, k_len, nq, nk, causal, scale, **more)
+    for s, (a, b) in enumerate(zip(nq, nk)):
+        q0, k0 = int(cu_q[s]), int(cu_k[s])
+        want, off = reference(q[q0:q0 + a], k[k0:k0 + b], v[k0:k0 + b], causal, scale)
+        got = out[q0:q0 + a].double()
+        assert bool(((got - want).abs() <= off).all()), (s, a, b, float(((got - want).abs() / off.clamp(min=1e-30)).nan_to_num(1e9).max()))
+    again = _run(cm, q, k, v, cu_q, cu_k, k_len, nq, nk, causal, scale, **more)
+    assert torch.equal(again[:sum(nq)], out[:sum(nq)])                     # no order of anything is left to chance
+    return out
+
+
+PROMPTS = [[1], [2], [63], [64], [65], [127], [128], [129], [191], [192], [193], [300], [1000], [2500], [77, 31, 1, 64, 0, 77, 12, 50], [0, 0, 5, 0],
+           [513, 200, 1, 640, 64], [129] * 9, [1] * 130, [700] + [3] * 70 + [400]]
+
+
+@gpu
+@pytest.mark.parametrize("lengths", PROMPTS, ids=lambda n: f"{len(n)}x{max(n)}")
+@pytest.mark.parametrize("E", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_prompts(cm, lengths, E, causal):
+    for dtype in TYPES:
+        _check(cm, lengths, lengths, 4, 2, E, dtype, causal, seed=len(lengths), packed=True)
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk", [(1, 1), (2, 1), (3, 3), (5, 1), (6, 6), (8, 8), (16, 8), (20, 4), (24, 24), (10, 2), (12, 3), (64, 8), (40, 40)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_heads(cm, Hq, Hk, causal):
+    _check(cm, [260, 7, 130], [260, 7, 130], Hq, Hk, 64, torch.bfloat16, causal)
+    _check(cm, [1, 1, 2], [260, 7, 130], Hq, Hk, 128, torch.float16, causal)
+
+
+CONTINUED = [([5], [70]), ([1], [1]), ([1], [64]), ([1], [65]), ([1, 1, 1], [1, 4000, 129]), ([17, 3], [200, 3]), ([150], [1000]), ([64, 0, 9], [64, 30, 0]),
+             ([300, 2], [100, 1]), ([200], [1]), ([4, 4, 4, 4], [4, 5, 600, 0]), ([1] * 40, list(range(0, 2000, 50))), ([130, 1, 33], [129, 900, 31]), ([8], [5000]), ([1], [9001])]
+
+
+@gpu
+@pytest.mark.parametrize("nq,nk", CONTINUED, ids=lambda n: f"{len(n)}x{max(n)}")
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("slot", [False, True])
+def test_more_or_fewer_keys_than_queries(cm, nq, nk, causal, slot):
+    """Caches with room, NaN behind what is in use; a causal query that sees no key gets zero."""
+    for dtype, (Hq, Hk), E in ((torch.bfloat16, (8, 2), 128), (torch.float16, (4, 4), 64)):
+        _check(cm, nq, nk, Hq, Hk, E, dtype, causal, seed=max(nk), slot=max(nk) + 3 if slot else 0)
+
+
+@gpu
+@pytest.mark.parametrize("nq", [1, 2, 3, 5, 8, 16, 17, 40])
+@pytest.mark.parametrize("G", [1, 3, 4, 8, 16])
+def test_few_queries(cm, nq, G):
+    _check(cm, [nq, nq, 1], [700, nq, 2111], 2 * G, 2, 128, torch.bfloat16, True, seed=G, slot=2200)
+    _check(cm, [nq, nq, 1], [700, nq, 2111], 2 * G, 2, 64, torch.float16, True, seed=G)
+
+
+@gpu
+@pytest.mark.parametrize("scale,size", [(3.0, 1.0), (1e-4, 1.0), (0.125, 30.0), (1.0, 0.01)])
+@pytest.mark.parametrize("E", [64, 128])
+def test_peaked_and_flat_rows(cm, scale, size, E):
+    """Scores into the hundreds, where one key has all the weight, and rows of equal weights."""
+    for dtype in TYPES:
+        _check(cm, [400, 1], [400, 1500], 2, 1, E, dtype, True, scale=scale, size=size)
+
+
+@gpu
+@pytest.mark.parametrize("E", [64, 128])
+@pytest.mark.parametrize("nq,nk", [([500, 300], [500, 300]), ([1, 1], [900, 300]), ([6, 3], [900, 300])])
+def test_rising_and_falling_scores(cm, E, nq, nk):
+    """The largest score last: the reference rises with every tile; first: it never does.  Far below zero all of them."""
+    for sign in (1.0, -1.0):
+        for shift in (0.0, -40.0):
+            q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, 2, 2, E, torch.bfloat16, 3)
+            q.fill_(0.5)
+            ramp = torch.cat([torch.linspace(0, 20, n) for n in nk]).to(DEV)
+            k.copy_((k.float() * 0.01 + sign * ramp[:, None, None] * 0.1 + shift).to(k.dtype))
+            out = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.25)
+            for s in range(2):
+                a, b = slice(int(cu_q[s]), int(cu_q[s + 1])), slice(int(cu_k[s]), int(cu_k[s + 1]))
+                want, off = reference(q[a], k[b], v[b], True, 0.25)
+                assert bool(((out[a].double() - want).abs() <= off).all())
+
+
+@gpu
+@pytest.mark.parametrize("nq,nk,at", [([200], [200], 150), ([200], [200], 64), ([300], [300], 0), ([5], [400], 397), ([1], [400], 399), ([3, 9], [100, 100], 98), ([64], [64], 63)])
+@pytest.mark.parametrize("kind", [math.nan, math.inf, -math.inf])
+def test_hidden_keys_have_no_influence(cm, nq, nk, at, kind):
+    """A key and value that hold an infinity or a NaN reach the queries that see them and no other."""
+    for dtype, E in ((torch.bfloat16, 128), (torch.float16, 64)):
+        q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, 4, 2, E, dtype, 5)
+        clean = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1)
+        row = int(cu_k[0]) + at
+        sees = (torch.arange(nq[0], device=DEV) + nk[0] - nq[0]) >= at
+        for spoiled in (k, v):
+            before = spoiled[row].clone()
+            spoiled[row, :, 5] = kind
+            out = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1)
+            spoiled[row] = before
+            assert torch.equal(out[:nq[0]][~sees], clean[:nq[0]][~sees]) and torch.equal(out[nq[0]:], clean[nq[0]:])
+            if spoiled is v:
+                others = [e for e in range(E) if e != 5]
+                assert torch.equal(out[..., others], clean[..., others])
+                seen = out[:nq[0]][sees][..., 5]
+                assert bool(seen.isnan().all() if math.isnan(kind) else (seen == kind).all())
+            elif math.isnan(kind):
+                assert bool(out[:nq[0]][sees].isnan().all())
+
+
+@gpu
+def test_minus_infinite_scores(cm):
+    """A key whose score is minus infinity has no weight, also where it stands in front of all others."""
+    q, k, v, cu_q, cu_k, _ = _inputs([70, 1], [70, 300], 2, 1, 64, torch.bfloat16, 9)
+    q.abs_().clamp_(min=0.1)
+    for s, n in ((0, 20), (1, 200)):
+        k[int(cu_k[s]):int(cu_k[s]) + n, :, 3] = -math.inf
+    out = _run(cm, q, k, v, cu_q, cu_k, None, [70, 1], [70, 300], False, 0.1)
+    for s, n in ((0, 20), (1, 200)):
+        a, b = slice(int(cu_q[s]), int(cu_q[s + 1])), slice(int(cu_k[s]) + n, int(cu_k[s + 1]))
+        want, off = reference(q[a], k[b], v[b], False, 0.1)
+        assert bool(((out[a].double() - want).abs() <= off).all())
+
+
+@gpu
+def test_rows_of_no_sequence_stay(cm):
+    nq, nk = [30, 70], [30, 70]
+    q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, 2, 2, 64, torch.bfloat16, 1)
+    grown = [torch.cat([t[:9], t, t[:40]]) for t in (q, k, v)]
+    out = torch.full_like(grown[0], 7.0)
+    _run(cm, *grown, cu_q + 9, cu_k + 9, None, nq, nk, True, 0.1, out=out)
+    assert bool((out[:9] == 7).all()) and bool((out[109:] == 7).all())
+    assert torch.equal(out[9:109], _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1))
+
+
+@gpu
+def test_longer_limits_than_needed(cm):
+    """max_q and max_k are upper limits: another limit is another way to divide the work, within the tolerance of either."""
+    for nq, nk in (([3, 1], [500, 2000]), ([100, 60], [100, 60])):
+        for more in (1, 10, 100):
+            _check(cm, nq, nk, 4, 2, 64, torch.float16, True, max_q=max(nq) * more, max_k=max(nk) * more)
+
+
+@gpu
+def test_heads_of_rows_and_other_strides(cm):
+    """[heads, rows, E] and rows inside wider ones, and an output with gaps that stay."""
+    for nq, nk in (([130, 40], [130, 40]), ([1, 3], [300, 77])):
+        q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, 4, 2, 128, torch.bfloat16, 2)
+        want = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1)
+        by_head = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v)]
+        assert torch.equal(_run(cm, *by_head, cu_q, cu_k, None, nq, nk, True, 0.1, out=torch.empty_like(by_head[0])), want)
+        wide = torch.full((q.shape[0], 6, 136), 3.0, dtype=q.dtype, device=DEV)
+        _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1, out=wide[:, 1:5, :128])
+        assert torch.equal(wide[:, 1:5, :128], want) and bool((wide[:, [0, 5]] == 3).all()) and bool((wide[..., 128:] == 3).all())
+
+
+@gpu
+@pytest.mark.parametrize("nq", [1, 70])
+def test_offsets_beyond_32_bits(cm, nq):
+    """A head whose keys span more than 2^32 bytes."""
+    E, nk, stride = 64, 2300, 1 << 20
+    rows = torch.zeros((nk * stride + 4 * E,), dtype=torch.bfloat16, device=DEV)
+    q, k, v, cu_q, cu_k, _ = _inputs([nq], [nk], 2, 1, E, torch.bfloat16, 4)
+    far_k, far_v = (rows[i * E:].as_strided((nk, 1, E), (stride, E, 1)) for i in range(2))
+    far_k.copy_(k)
+    far_v.copy_(v)
+    assert torch.equal(_run(cm, q, far_k, far_v, cu_q, cu_k, None, [nq], [nk], True, 0.1), _run(cm, q, k, v, cu_q, cu_k, None, [nq], [nk], True, 0.1))
+
+
+@gpu
+def test_on_another_stream_and_in_graphs(cm):
+    """Two captured graphs with a workspace each, replayed by turns."""
+    calls = []
+    for nq, nk in (([1, 2, 1], [3000, 900, 20]), ([1, 1], [50, 2500])):
+        q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, 8, 2, 128, torch.bfloat16, len(nq))
+        ws = torch.empty(max(16, cm.attn_packed_workspace_bytes(len(nq), 8, 2, 128, 2, 3000)), dtype=torch.uint8, device=DEV)
+        calls.append((q, k, v, cu_q, cu_k, torch.zeros_like(q), ws))
+    graphs = []
+    for q, k, v, cu_q, cu_k, out, ws in calls:
+        cm.attn_packed(q, k, v, cu_q, cu_k, out, 2, 3000, True, 0.1, ws=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cm.attn_packed(q, k, v, cu_q, cu_k, out, 2, 3000, True, 0.1, ws=ws)
+        graphs.append(graph)
+    for turn in range(3):
+        for (q, k, v, cu_q, cu_k, out, ws), graph in zip(calls, graphs):
+            k.mul_(0.9)
+            out.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        for q, k, v, cu_q, cu_k, out, ws in calls:
+            want, side = torch.empty_like(out), torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                cm.attn_packed(q, k, v, cu_q, cu_k, want, 2, 3000, True, 0.1, ws=torch.empty_like(ws))
+            side.synchronize()
+            assert torch.equal(out, want)
+
+
+@gpu
+def test_bad_starts_stay_inside(cm):
+    """Entries outside the tensors, and descending ones: some result, and nothing outside the tensors is read or written."""
+    q, k, v, cu_q, cu_k, _ = _inputs([40, 40], [40, 40], 2, 1, 64, torch.bfloat16, 1)
+    frame = torch.full((120, 2, 64), 5.0, dtype=q.dtype, device=DEV)
+    for bad in ([-7, 30, 90], [50, 20, 10], [0, 2 ** 31 - 1, -2 ** 31], [79, 80, 81]):
+        starts = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        for lens in (None, torch.tensor([1000, -3], dtype=torch.int32, device=DEV)):
+            cm.attn_packed(q, k, v, starts, starts, frame[20:100], 80, 80, True, 0.1, k_len=lens)
+            cm.attn_packed(q, k, v, starts, starts, frame[20:100], 1, 80, True, 0.1, k_len=lens, ws=torch.empty(1 << 20, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert bool((frame[:20] == 5).all()) and bool((frame[100:] == 5).all())
+
+
+# ---- refusals (no GPU) ------------------------------------------------------------------------------------------------------
+
+def test_refuses(cm):
+    f, a = cm.load().chipmunk_attn_packed, ctypes.c_void_p(0x1000)
+
+    def call(q=a, qt=512, qh=64, k=a, kt=256, kh=64, v=a, vt=256, vh=64, out=a, ot=512, oh=64, cu_q=a, cu_k=a, k_len=a, S=2, Tq=100, Tk=100, Hq=8, Hk=4, E=64,
+             max_q=100, max_k=100, causal=1, scale=0.1, dtype=0, ws=a, ws_bytes=1 << 30):
+        return f(q, qt, qh, k, kt, kh, v, vt, vh, out, ot, oh, cu_q, cu_k, k_len, S, Tq, Tk, Hq, Hk, E, max_q, max_k, causal, scale, dtype, ws, ws_bytes, None)
+    for missing in ("q", "k", "v", "out", "cu_q", "cu_k"):
+        assert call(**{missing: None}) == -1
+    for wrong in (dict(S=0), dict(Tq=0), dict(Tk=0), dict(Hq=0), dict(Hk=0), dict(Hq=9), dict(Hq=2), dict(max_q=0), dict(max_k=-1), dict(scale=0.0), dict(scale=-1.0),
+                  dict(scale=math.nan), dict(scale=math.inf), dict(qt=56), dict(kt=0), dict(vt=-256), dict(ot=1 << 24), dict(kt=1 << 24), dict(qh=56), dict(vh=0),
+                  dict(S=1 << 22, Hq=64, qt=4096, ot=4096, max_q=1 << 20, Tq=1 << 30)):
+        assert call(**wrong) == -2, wrong
+    for wrong in (dict(E=96), dict(E=256), dict(dtype=2), dict(dtype=-1)):
+        assert call(**wrong) == -4, wrong
+    for wrong in (dict(q=ctypes.c_void_p(0x1008)), dict(k=ctypes.c_void_p(0x1004)), dict(v=ctypes.c_void_p(0x1002)), dict(out=ctypes.c_void_p(0x1008)),
+                  dict(cu_q=ctypes.c_void_p(0x1002)), dict(k_len=ctypes.c_void_p(0x1001)), dict(qt=516), dict(oh=68), dict(kh=68)):
+        assert call(**wrong) == -3, wrong
+
+
+def test_function_refuses(cm):
+    bf, i32 = torch.bfloat16, torch.int32
+    q, k, cu = torch.zeros(4, 2, 64, dtype=bf), torch.zeros(4, 1, 64, dtype=bf), torch.zeros(2, dtype=i32)
+    for args, error in (((q.float(), k, k, cu, cu, q, 4, 4, True, 0.1), TypeError), ((q, k, k, cu, cu, q, 4, 4, True, 0.1), ValueError), ((q, k.half(), k, cu, cu, q, 4, 4, True, 0.1), (TypeError, ValueError))):
+        with pytest.raises(error):
+            cm.attn_packed(*args)
+
+
+@gpu
+def test_function_refuses_on_the_gpu(cm):
+    bf, i32 = torch.bfloat16, torch.int32
+    q, k, cu = torch.zeros(4, 2, 64, dtype=bf, device=DEV), torch.zeros(4, 1, 64, dtype=bf, device=DEV), torch.tensor([0, 4], dtype=i32, device=DEV)
+    wrong = [(q, k.half(), k, cu, cu, q), (q, k, k[:3], cu, cu, q), (q, k[..., :32], k[..., :32], cu, cu, q), (q, k, k, cu.long(), cu, q), (q, k, k, cu, cu[:1], q),
+             (q, k, k, cu, cu, q[:3]), (q[0], k, k, cu, cu, q), (q, k, k, cu.cpu(), cu, q), (q, k, k, cu, cu, q.half()), (q[..., ::2], k, k, cu, cu, q)]
+    for args in wrong:
+        with pytest.raises((TypeError, ValueError)):
+            cm.attn_packed(*args, 4, 4, True, 0.1)
+    with pytest.raises((TypeError, ValueError)):
+        cm.attn_packed(q, k, k, cu, cu, torch.empty_like(q), 4, 4, True, 0.1, k_len=cu)
+    for scale in (0.0, math.nan):
+        with pytest.raises(cm.ChipmunkError):
+            cm.attn_packed(q, k, k, cu, cu, torch.empty_like(q), 4, 4, True, scale)
