@@ -84,10 +84,11 @@ def _check_linear(cm, N, D, F, dtype, act, bias=True, residual=True, seed=0, spr
 SIZES = [(1, 8, 8), (1, 264, 72), (2, 256, 5120), (3, 4096, 1000), (5, 72, 16), (15, 1032, 520), (16, 640, 136), (17, 2056, 264), (31, 512, 2048),
          (33, 4104, 88), (64, 1024, 1024), (65, 64, 64), (100, 5120, 24), (127, 576, 392), (200, 8, 640), (255, 1536, 768), (256, 256, 256),
          (257, 320, 2056), (500, 3000, 1288), (1000, 128, 5000), (2049, 1000, 2000), (4608, 640, 1920)]
+MORE_SIZES = [(100, 1040, 13392), (380, 392, 10880), (900, 4360, 2544), (450, 200, 10880), (2100, 968, 8200), (1500, 1016, 3000), (513, 72, 12296), (33, 8200, 264)]
 
 
 @gpu
-@pytest.mark.parametrize("N,D,F", SIZES)
+@pytest.mark.parametrize("N,D,F", SIZES + MORE_SIZES)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear(cm, N, D, F, dtype):
     seed = N + D + F
@@ -174,6 +175,38 @@ def test_linear_beyond_32_bits(cm):
     cm.linear(x, w, None, None, out)
     want, off = linear_reference(x.contiguous(), w, None, None, 2)
     assert bool(((out.double() - want).abs() <= off).all())
+
+
+def test_every_form_of_tiles_is_reached(cm):
+    """From one row to thousands; the sizes of test_linear take each form."""
+    form = cm.load().chipmunk_internal_linear_form
+    assert form(1, 4096, 4096) == form(16, 64, 30720) == form(32, 4096, 4096) == 7 and form(17, 4096, 30720) < 7
+    assert {form(N, D, F) for N, D, F in SIZES + MORE_SIZES} == set(range(8))
+
+
+def test_no_accumulator_is_touched_before_its_product_has_landed(tmp_path):
+    """The widest tiles' products are inline assembly (see the module of the same check)."""
+    import os
+    import re
+    import subprocess
+
+    from paper_2506_03275_amd import build
+    from test_compiled_products import _faults
+    out = tmp_path / "linear.s"
+    flags = [f for f in build.HIPCC_FLAGS if f != "-shared"]
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "--offload-device-only", "-S", os.path.join(build.CSRC, "linear.hip"), "-o", str(out)],
+                   check=True, capture_output=True)
+    text = out.read_text()
+    kernels = re.findall(r"^(_ZN\w*linear_wide_kernel\w*):(.*?)^\s*\.size\s+\1,", text, re.S | re.M)
+    assert len(kernels) == 4   # two types, a whole or a cut last step
+    for name, body in kernels:
+        lines = [line.split(";")[0].strip() for line in body.split("\n")]
+        assert not _faults([line for line in lines if line and not re.match(r"\.(?!L)", line)]), name
+    # in scratch memory: some of the widest tiles' accumulators, behind the loop, which the check above looked at
+    spills = dict(re.findall(r"\.name:\s+(_ZN\w*linear_\w+_kernel\w*).*?\.vgpr_spill_count:\s*(\d+)", text, re.S))
+    assert len(spills) >= 20
+    for name, n in spills.items():
+        assert int(n) <= (0 if "wide" not in name else 28 if "Fp16" in name else 1), (name, n)
 
 
 # ---- rotary positions ---------------------------------------------------------------------------------------------------
