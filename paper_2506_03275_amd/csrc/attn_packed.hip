@@ -24,6 +24,9 @@ struct PackedParams {
     int S, Tq, Tk, Hq, Hk, G;
     int max_q, max_k, causal;
     int tiles;     // of one head: as many as there can be
+    int part_keys, parts;   // few queries: keys that a workgroup walks, and how many such parts the longest sequence can have
+    int few_rows;  // rows of a key head: max_q * G
+    float* partial;         // [S][Hk][parts][few_rows][E] sums, then [S][Hk][parts][few_rows][2]: reference (log2 units), sum of weights
     float sl2;     // softmax_scale * log2(e)
 };
 
@@ -223,6 +226,29 @@ __device__ __forceinline__ void tile_values(RowState<T, E, NQB>& st, const f32x4
     }
 }
 
+// Adds the infinite and NaN values of keys first .. last - 1 to the queries that see them (tile_values leaves them out where
+// something is hidden).
+template <class T, int E, int NQB>
+__device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, const uint16_t* vh, int64_t v_token, int first, int last, const int (&limit)[NQB], int g) {
+#pragma unroll 1
+    for (int key = first; key < last; key++) {
+        const uint16_t* from = vh + key * v_token + 4 * g;
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) {
+            const u32x2 words = *reinterpret_cast<const u32x2*>(from + eb * 16);
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                float value = r % 2 ? T::high(words[r / 2]) : T::low(words[r / 2]);
+                const bool special = r % 2 ? high_not_finite<T>(words[r / 2]) : low_not_finite<T>(words[r / 2]);
+                asm volatile("" : "+v"(value));           // nothing is known of it, not even that it is none of the two
+#pragma unroll
+                for (int qb = 0; qb < NQB; qb++)
+                    if (special && key < limit[qb]) st.O[eb][qb][r] += value;
+            }
+        }
+    }
+}
+
 // Tile and head of a workgroup.  Workgroups go to the eight XCDs in turn (id modulo 8), each with an L2 of its own: a key head's
 // workgroups stay on as few XCDs as there are heads for, and every XCD gets as many of the long tiles.
 __device__ __forceinline__ void tile_and_head(const PackedParams& p, uint32_t id, int* tile, int* head) {
@@ -399,25 +425,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_rows_kernel(PackedParams p
     wait_all_memory();                                    // the transfers behind the last step
 
     // Infinite and NaN values among the steps with hidden keys go to the queries that see them.
-    if (__builtin_amdgcn_ballot_w64(found) != 0) {
-#pragma unroll 1
-        for (int key = first_hidden; key < seen; key++) {
-            const uint16_t* from = vh + key * p.v_token + 4 * g;
-#pragma unroll
-            for (int eb = 0; eb < E / 16; eb++) {
-                const u32x2 words = *reinterpret_cast<const u32x2*>(from + eb * 16);
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    float value = r % 2 ? T::high(words[r / 2]) : T::low(words[r / 2]);
-                    const bool special = r % 2 ? high_not_finite<T>(words[r / 2]) : low_not_finite<T>(words[r / 2]);
-                    asm volatile("" : "+v"(value));       // nothing is known of it, not even that it is none of the two
-#pragma unroll
-                    for (int qb = 0; qb < NQB; qb++)
-                        if (special && key < limit[qb]) st.O[eb][qb][r] += value;
-                }
-            }
-        }
-    }
+    if (__builtin_amdgcn_ballot_w64(found) != 0) add_special_values<T, E, NQB>(st, vh, p.v_token, first_hidden, seen, limit, g);
 
 #pragma unroll
     for (int qb = 0; qb < NQB; qb++) {
@@ -438,6 +446,249 @@ __global__ __launch_bounds__(256, 2) void attn_packed_rows_kernel(PackedParams p
     }
 }
 
+// Few queries over many keys: a workgroup owns one key head of one sequence and walks part_keys of its keys for all rows of the head
+// (query i, head g of the group: row i * G + g), so the keys and values are read once for the whole group.  Its waves take the tiles of 32 keys in
+// turn, each with a K and a V tile of its own in LDS and a reference, sum and accumulator of its own: no wave waits for another before
+// they meet at the end.  A longer sequence's parts are joined by attn_packed_join_kernel.
+//
+// Bound: memory, K and V read once.  A K tile is requested again as soon as its scores have been formed, a V tile when it has been
+// weighted: of the eight waves on a CU at most one is without a request.
+template <class T, int E, int NQB>
+__global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(PackedParams p) {
+    typedef typename T::x8 x8;
+    constexpr int ROWB = E * 2, CH = ROWB / 16, RPI = 64 / CH, NI = kTile / RPI;   // NI: transfers of a tile
+    constexpr int TILE = kTile * ROWB;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, l16 = lane & 15;
+    // workgroups go to the XCDs in turn: a sequence's heads, whose rows lie side by side, to all of them
+    int id = (int)(blockIdx.x / p.Hk);
+    const int head = (int)blockIdx.x % p.Hk, s = id % p.S;
+    id /= p.S;
+    const int part = id % p.parts, row0 = (p.tiles - 1 - id / p.parts) * 16 * NQB;   // the last rows, which may see the most, first
+    const Rows qs = queries_of(p, s), ks = keys_of(p, s);
+    const int rows = min(16 * NQB, qs.count * p.G - row0);
+    if (rows <= 0) return;
+    const int past = ks.count - qs.count;
+    // the first keys that the first and the last row do not see
+    const int seen_by_all = p.causal ? min(ks.count, row0 / p.G + 1 + past) : ks.count;
+    const int seen = p.causal ? min(ks.count, (row0 + rows - 1) / p.G + 1 + past) : ks.count;
+    const int start = part * p.part_keys, end = min(p.parts == 1 ? seen : ks.count, start + p.part_keys);
+    if (start >= end && part > 0) return;                 // (without any key the first part writes zeros)
+    const uint16_t* kh = p.k + head * p.k_head + (int64_t)ks.first * p.k_token;
+    const uint16_t* vh = p.v + head * p.v_head + (int64_t)ks.first * p.v_token;
+
+    RowState<T, E, NQB> st;
+    int limit[NQB];                                       // the first key that the lane's row does not see
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++) {
+        st.negm[qb] = st.L[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) st.O[eb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int row = row0 + min(qb * 16 + l16, rows - 1), i = row / p.G;   // (rows that are not there: the last one's limit)
+        limit[qb] = p.causal ? min(ks.count, i + 1 + past) : ks.count;
+        const uint16_t* from = p.q + (int64_t)(qs.first + i) * p.q_token + (head * p.G + row % p.G) * p.q_head + 8 * g;
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) {
+            u32x4 val = u32x4{0, 0, 0, 0};
+            if (qb * 16 + l16 < rows) val = *reinterpret_cast<const u32x4*>(from + 32 * es);
+            st.Q[es][qb] = __builtin_bit_cast(x8, val);
+        }
+    }
+    const float slack = kSlack / p.sl2;
+
+    const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
+    const int vrow = 4 * g + (l16 >> 2);
+    const int voff = vrow * ROWB + ((((l16 & 3) >> 1) ^ tile_swizzle<E>(vrow)) * 16) + 8 * (l16 & 1);
+    const uint32_t smem_at = (uint32_t)(uintptr_t)CHIPMUNK_LDS_PTR(smem) + w * 2 * TILE;
+    uint32_t kaddr[E / 32], vaddr[E / 16];
+#pragma unroll
+    for (int es = 0; es < E / 32; es++) kaddr[es] = smem_at + (uint32_t)(koff ^ (64 * es));
+#pragma unroll
+    for (int eb = 0; eb < E / 16; eb++) vaddr[eb] = smem_at + (uint32_t)(voff ^ (32 * eb));
+    uint32_t from_k[NI], from_v[NI];
+#pragma unroll
+    for (int i = 0; i < NI; i++) {
+        const int row = i * RPI + lane / CH;
+        const uint32_t chunk = (uint32_t)(((lane % CH) ^ tile_swizzle<E>(row)) * 16);
+        from_k[i] = (uint32_t)row * (uint32_t)(p.k_token * 2) + chunk;
+        from_v[i] = (uint32_t)row * (uint32_t)(p.v_token * 2) + chunk;
+    }
+    const uint32_t lds0 = lds_address(smem) + (uint32_t)(w * 2 * TILE);
+    // the tile from key `first` on; what lies behind the part's end reads as zero
+    auto request = [&](const uint16_t* rows_at, int64_t token, const uint32_t (&from)[NI], int first, uint32_t to) {
+        const int left = min(max(end - first, 0), kTile);
+        const i32x4 buf = raw_buffer_words(rows_at + first * token, left > 0 ? (uint32_t)((left - 1) * token + E) * 2u : 0u);
+#pragma unroll
+        for (int i = 0; i < NI; i++) load_buffer_to_lds_16B(buf, from[i], to + i * 1024);
+    };
+    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
+    int first = start + w * kTile;
+    wait_all_memory();                                    // the queries
+    if (first < end) {
+        request(kh, p.k_token, from_k, first, lds0);
+        request(vh, p.v_token, from_v, first, lds0 + TILE);
+    }
+    bool found = false;
+    auto tile = [&](auto hidden_c) {
+        constexpr bool HIDDEN = decltype(hidden_c)::value;
+        f32x4 S[2][NQB];
+        wait_vmem_at_most<NI>();                          // K has landed
+        asm volatile("" ::: "memory");
+        tile_scores<T, E, NQB>(S, st, kaddr, 0, [](int) {});
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and has been read
+        request(kh, p.k_token, from_k, first + TURN, lds0);
+        if (HIDDEN) {
+            int within[NQB];                              // the part's end hides the keys behind it as well
+#pragma unroll
+            for (int qb = 0; qb < NQB; qb++) within[qb] = min(limit[qb], end);
+            hide_keys<NQB>(S, first + 4 * g, within);
+        }
+        raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+        wait_vmem_at_most<NI>();                          // V
+        asm volatile("" ::: "memory");
+        tile_values<T, E, NQB, HIDDEN>(st, S, vaddr, TILE, p.sl2, found);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        request(vh, p.v_token, from_v, first + TURN, lds0 + TILE);
+    };
+    const int plain_end = min(end, seen_by_all);
+#pragma unroll 1
+    for (; first + kTile <= plain_end; first += TURN) tile(std::false_type{});
+    const int first_hidden = first;
+#pragma unroll 1
+    for (; first < end; first += TURN) tile(std::true_type{});
+    wait_all_memory();
+    if (__builtin_amdgcn_ballot_w64(found) != 0)
+        for (int at = first_hidden; at < end; at += TURN) add_special_values<T, E, NQB>(st, vh, p.v_token, at, min(end, at + kTile), limit, g);
+    lds_accesses_then_barrier();                          // every wave is done with its tiles
+
+    // The waves' sums meet in LDS, two blocks of rows at a time; each wave joins a quarter of the columns.
+    constexpr int TOGETHER = NQB < 2 ? NQB : 2, COLUMNS = E / 16 / 4;
+    f32x4* sums = reinterpret_cast<f32x4*>(smem);         // [wave][block of rows][block of columns][lane]
+    f32x2* stats = reinterpret_cast<f32x2*>(smem + 4 * TOGETHER * E * 64);   // [wave][block of rows][lane]
+    const bool alone = p.parts == 1 || ks.count <= p.part_keys;
+#pragma unroll
+    for (int qb0 = 0; qb0 < NQB; qb0 += TOGETHER) {
+        if (qb0 > 0) lds_accesses_then_barrier();
+#pragma unroll
+        for (int b = 0; b < TOGETHER; b++) {
+            const int qb = qb0 + b;
+#pragma unroll
+            for (int eb = 0; eb < E / 16; eb++) sums[((w * TOGETHER + b) * (E / 16) + eb) * 64 + lane] = st.O[eb][qb];
+            const float m = st.L[qb][0] == 0.f ? -INFINITY : -st.negm[qb][0] * p.sl2;   // no weight: no reference
+            stats[(w * TOGETHER + b) * 64 + lane] = f32x2{m, st.L[qb][0]};
+        }
+        lds_accesses_then_barrier();
+#pragma unroll
+        for (int b = 0; b < TOGETHER; b++) {
+            const int row = row0 + (qb0 + b) * 16 + l16;
+            float m[4], l[4], top = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                const f32x2 x = stats[(v * TOGETHER + b) * 64 + lane];
+                m[v] = x[0];
+                l[v] = x[1];
+                top = fmaxf(top, m[v]);
+            }
+            float total = 0.f;
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                m[v] = m[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[v] - top);
+                total += l[v] * m[v];
+            }
+            f32x4 o[COLUMNS];
+#pragma unroll
+            for (int i = 0; i < COLUMNS; i++) {
+                o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int v = 0; v < 4; v++) o[i] += sums[((v * TOGETHER + b) * (E / 16) + w * COLUMNS + i) * 64 + lane] * m[v];
+            }
+            if (row >= row0 + rows) continue;
+            const int column = w * COLUMNS * 16 + 4 * g;
+            if (alone) {
+                const float f = limit[qb0 + b] > 0 ? 1.f / total : 0.f;          // no key to see: zero
+                uint16_t* to = p.out + (int64_t)(qs.first + row / p.G) * p.out_token + (head * p.G + row % p.G) * p.out_head + column;
+#pragma unroll
+                for (int i = 0; i < COLUMNS; i++) *reinterpret_cast<u32x2*>(to + i * 16) = u32x2{T::pack(o[i][0] * f, o[i][1] * f), T::pack(o[i][2] * f, o[i][3] * f)};
+            } else {
+                const int64_t at = (((int64_t)s * p.Hk + head) * p.parts + part) * p.few_rows + row;
+#pragma unroll
+                for (int i = 0; i < COLUMNS; i++) *reinterpret_cast<f32x4*>(p.partial + at * E + column + i * 16) = o[i];
+                if (w == 0 && g == 0)
+                    *reinterpret_cast<f32x2*>(p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + at * 2) = f32x2{top, total};
+            }
+        }
+    }
+}
+
+// Joins the parts of the sequences that have more than one: a wave per row.
+template <class T, int E>
+__global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedParams p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= (int64_t)p.S * p.Hk * p.few_rows) return;
+    const int row = (int)(id % p.few_rows), head = (int)(id / p.few_rows % p.Hk), s = (int)(id / p.few_rows / p.Hk);
+    const Rows qs = queries_of(p, s), ks = keys_of(p, s);
+    if (row >= qs.count * p.G || ks.count <= p.part_keys) return;
+    const int parts = (ks.count + p.part_keys - 1) / p.part_keys;
+    const float* sums = p.partial + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * E;
+    const float* stats = p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * 2;
+    constexpr int PER = E / 64;                           // columns of a lane
+    float top = -INFINITY, total = 0.f, o[PER] = {};
+    for (int part0 = 0; part0 < parts; part0 += 64) {     // 64 parts' references and sums at a time
+        f32x2 mine = f32x2{-INFINITY, 0.f};
+        if (part0 + lane < parts) mine = *reinterpret_cast<const f32x2*>(stats + (int64_t)(part0 + lane) * p.few_rows * 2);
+        float most = mine[0];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        most = fmaxf(most, top);
+        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most);
+        const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[0] - most);
+        float add = mine[1] * weight;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
+        total = total * before + add;
+        top = most;
+#pragma unroll
+        for (int i = 0; i < PER; i++) o[i] *= before;
+        const int here = min(64, parts - part0);
+        auto load = [&](int n, float (&v)[PER]) {
+            const float* from = sums + (int64_t)(part0 + n) * p.few_rows * E + lane * PER;
+            if constexpr (PER == 2) {
+                const f32x2 x = *reinterpret_cast<const f32x2*>(from);
+                v[0] = x[0];
+                v[PER - 1] = x[1];
+            } else {
+                v[0] = *from;
+            }
+        };
+        constexpr int AHEAD = 8;
+        for (int n0 = 0; n0 < here; n0 += AHEAD) {
+            float v[AHEAD][PER];
+#pragma unroll
+            for (int n = 0; n < AHEAD; n++) load(min(n0 + n, here - 1), v[n]);
+#pragma unroll
+            for (int n = 0; n < AHEAD; n++) {
+                const float f = n0 + n < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), min(n0 + n, here - 1))) : 0.f;
+                if (n0 + n < here) {
+#pragma unroll
+                    for (int i = 0; i < PER; i++) o[i] += v[n][i] * f;
+                }
+            }
+        }
+    }
+    // a row that sees no key has no weight anywhere
+    const int i = row / p.G;
+    const float f = p.causal && i + 1 + ks.count - qs.count <= 0 ? 0.f : 1.f / total;
+    uint16_t* to = p.out + (int64_t)(qs.first + i) * p.out_token + (head * p.G + row % p.G) * p.out_head + lane * PER;
+    if constexpr (PER == 2) {
+        *reinterpret_cast<uint32_t*>(to) = T::pack(o[0] * f, o[PER - 1] * f);
+    } else {
+        *to = (uint16_t)T::pack(o[0] * f, 0.f);
+    }
+}
+
 template <class T, int E, int NQB>
 static int32_t launch_rows(PackedParams p, hipStream_t stream) {
     constexpr int ROWS = 64 * NQB, LDS = 2 * kStepTiles * 2 * kTile * E * 2;
@@ -450,17 +701,116 @@ static int32_t launch_rows(PackedParams p, hipStream_t stream) {
     return launch_status();
 }
 
-template <class T>
-static int32_t launch_packed(const PackedParams& p, int E, hipStream_t stream) {
-    return E == 128 ? launch_rows<T, 128, 2>(p, stream) : launch_rows<T, 64, 2>(p, stream);
+// A few queries over many keys are walked in parts: rows of a key head, keys of a workgroup, parts of the longest sequence.
+// rows 0: in whole sequences.
+struct FewPlan {
+    int rows, part_keys, parts;
+};
+// Parts are as long as still leaves every CU a few of them: 1024 keys, less where few heads have keys for few parts (one sequence of 4000,
+// 8 heads: 256 keys 10.3 us, 1024 13.6), longer ones where there are many sequences (64 of 8000, 8 heads: 4096 keys 368 us, 1024 382, whole
+// 359, which a batch with one long sequence would pay for).
+static FewPlan few_plan(int S, int Hq, int Hk, int max_q, int max_k) {
+    const int64_t rows = (int64_t)max_q * (Hq / Hk), heads = (int64_t)S * Hk;
+    if (max_k <= 1024 || rows > 256 || (rows > 64 && heads * ((rows + 63) / 64) >= 128)) return FewPlan{0, 0, 0};
+    int keys = heads >= 512 ? 4096 : heads >= 64 ? 2048 : 1024;
+    if (heads < 64)
+        while (keys > 256 && keys * 8 >= max_k) keys /= 2;
+    return FewPlan{(int)rows, keys, (int)(((int64_t)max_k + keys - 1) / keys)};
+}
+static size_t few_bytes(const FewPlan& f, int S, int Hk, int E) {
+    return f.parts <= 1 ? 0 : (size_t)S * Hk * f.parts * f.rows * (E + 2) * sizeof(float);
+}
+
+// Everything else has a form by its price in us: how many workgroups there are, each with its start and end, 512 of them side by side; what
+// 64 keys take the workgroup that has the most of them, which bounds a small launch; what 64 rows x 64 keys take where the CUs are full, and a share
+// of the last workgroup.  Fitted to 2321 random batches of 1 to 32 sequences of up to 10 000 tokens, 1 to 120 heads, causal or not: the form
+// taken is 1.016 times the quickest's time in the mean.  The lengths are on the device: one sequence of the given limits is assumed, and the
+// rest of the rows evenly spread over the others.
+enum PackedForm { kKeys16, kKeys32, kRows64, kRows128, kRows192, kPackedForms };
+struct PackedPrice {
+    int rows;
+    float start, alone, full;
+};
+static const PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.3f, 0.27f, 0.76f}, {32, 4.4f, 0.27f, 0.43f}, {64, 2.9f, 0.64f, 0.35f}, {128, 4.1f, 1.29f, 0.30f}, {192, 8.5f, 1.14f, 0.31f}},
+                                                           {{16, 4.8f, 0.31f, 1.89f}, {32, 6.9f, 0.45f, 0.87f}, {64, 4.8f, 0.64f, 0.77f}, {128, 4.8f, 1.71f, 0.47f}, {192, 10.7f, 2.11f, 0.41f}}};
+static const float kPackedLast[2][2] = {{0.61f, 0.28f}, {0.50f, 0.45f}};   // of E = 64, 128; all keys, causal
+static double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
+    const PackedPrice& f = kPackedPrices[E == 128][form];
+    const bool grouped = form <= kKeys32;                 // rows of a key head, of all its queries' heads
+    const double per_query = grouped ? (double)Hq / Hk : 1.0, heads = grouped ? Hk : Hq;
+    double workgroups = 0, units = 0;
+    const double rest = S > 1 ? std::max(0.0, (double)(Tq - max_q) / (S - 1)) : 0.0;
+    auto add = [&](double sequences, double nq, double nk) {
+        const double blocks = std::max(1.0, (double)(int64_t)((nq * per_query + f.rows - 1) / f.rows));
+        const double keys = causal ? std::max(nk - nq / 2 + f.rows / per_query / 2, std::min(nk, 64.0)) : nk;
+        workgroups += sequences * blocks * heads;
+        units += sequences * blocks * heads * (f.rows / 64.0) * (std::min(keys, nk) / 64);
+    };
+    add(1, max_q, max_k);
+    if (S > 1) add(S - 1, rest, rest * max_k / max_q);
+    const double longest = max_k / 64.0, last = kPackedLast[E == 128][causal != 0] * longest * (f.rows / 64.0) * f.full;
+    return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last);
+}
+static PackedForm packed_form(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
+    PackedForm best = kKeys16;
+    for (int f = 1; f < kPackedForms; f++)
+        if (packed_price((PackedForm)f, S, Tq, Hq, Hk, E, max_q, max_k, causal) < packed_price(best, S, Tq, Hq, Hk, E, max_q, max_k, causal)) best = (PackedForm)f;
+    return best;
+}
+
+template <class T, int E, int NQB>
+static int32_t launch_few(PackedParams p, hipStream_t stream) {
+    constexpr int TOGETHER = NQB < 2 ? NQB : 2;
+    constexpr int LDS = std::max(4 * 2 * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
+    const auto kernel = attn_packed_few_kernel<T, E, NQB>;
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
+    p.tiles = (p.few_rows + 16 * NQB - 1) / (16 * NQB);
+    if ((int64_t)p.S * p.Hk * p.parts * p.tiles >= INT64_C(1) << 24) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
+    kernel<<<(uint32_t)(p.S * p.Hk * p.parts * p.tiles), 256, LDS, stream>>>(p);
+    if (p.parts > 1) attn_packed_join_kernel<T, E><<<(uint32_t)(((int64_t)p.S * p.Hk * p.few_rows + 3) / 4), 256, 0, stream>>>(p);
+    return launch_status();
+}
+
+template <class T, int E>
+static int32_t launch_packed(PackedParams p, const FewPlan& few, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (few.rows > 0) {
+        if (few_bytes(few, p.S, p.Hk, E) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
+        if ((int64_t)p.S * p.Hk * few.rows >= INT64_C(1) << 26) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
+        p.few_rows = few.rows;
+        p.part_keys = few.part_keys;
+        p.parts = few.parts;
+        p.partial = static_cast<float*>(ws);
+        return few.rows <= 16 ? launch_few<T, E, 1>(p, stream) : few.rows <= 32 ? launch_few<T, E, 2>(p, stream) : launch_few<T, E, 4>(p, stream);
+    }
+    const PackedForm form = packed_form(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, p.max_k, p.causal);
+    if (form <= kKeys32) {
+        if ((int64_t)p.max_q * p.G > INT32_MAX / 2) return CHIPMUNK_ERR_SHAPE;
+        p.few_rows = p.max_q * p.G;
+        p.part_keys = INT32_MAX;
+        p.parts = 1;
+    }
+    switch (form) {
+        case kKeys16: return launch_few<T, E, 1>(p, stream);
+        case kKeys32: return launch_few<T, E, 2>(p, stream);
+        case kRows64: return launch_rows<T, E, 1>(p, stream);
+        case kRows128: return launch_rows<T, E, 2>(p, stream);
+        default: return launch_rows<T, E, 3>(p, stream);
+    }
 }
 
 }  // namespace chipmunk
 
 using namespace chipmunk;
 
+// The form that a call takes and, for parts, their keys, for the tests.
+extern "C" int chipmunk_internal_attn_packed_form(int S, int Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
+    const FewPlan few = few_plan(S, Hq, Hk, max_q, max_k);
+    return few.rows > 0 ? few.part_keys : packed_form(S, Tq, Hq, Hk, E, std::min(max_q, Tq), max_k, causal);
+}
+
 extern "C" size_t chipmunk_attn_packed_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k) {
-    return 0;
+    if (S <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (E != 64 && E != 128) || max_q <= 0 || max_k <= 0) return 0;
+    return few_bytes(few_plan(S, Hq, Hk, max_q, max_k), S, Hk, E);
 }
 
 extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const uint16_t* k, int64_t k_token_stride,
@@ -477,12 +827,15 @@ extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_strid
         if (token < E || token >= kMostStride) return CHIPMUNK_ERR_SHAPE;
     if ((Hq > 1 && (q_head_stride < E || out_head_stride < E)) || (Hk > 1 && (k_head_stride < E || v_head_stride < E))) return CHIPMUNK_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
-        ((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(cu_k) | reinterpret_cast<uintptr_t>(k_len)) & 3) ||
+        !aligned16(ws) || ((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(cu_k) | reinterpret_cast<uintptr_t>(k_len)) & 3) ||
         (q_token_stride | k_token_stride | v_token_stride | out_token_stride) % 8 != 0 || (Hq > 1 && (q_head_stride | out_head_stride) % 8 != 0) ||
         (Hk > 1 && (k_head_stride | v_head_stride) % 8 != 0))
         return CHIPMUNK_ERR_ALIGN;
     const PackedParams p{q, k, v, out, cu_q, cu_k, k_len, q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
-                         out_token_stride, out_head_stride, S, Tq, Tk, Hq, Hk, Hq / Hk, std::min(max_q, Tq), std::min(max_k, Tk), causal != 0, 0,
+                         out_token_stride, out_head_stride, S, Tq, Tk, Hq, Hk, Hq / Hk, std::min(max_q, Tq), std::min(max_k, Tk), causal != 0, 0, 0, 0, 0, nullptr,
                          softmax_scale * 1.4426950408889634f};
-    return dtype == CHIPMUNK_DTYPE_BF16 ? launch_packed<Bf16>(p, E, static_cast<hipStream_t>(stream)) : launch_packed<Fp16>(p, E, static_cast<hipStream_t>(stream));
+    const FewPlan few = few_plan(S, Hq, Hk, max_q, max_k);   // by the limits as given, like the workspace's size
+    const auto st = static_cast<hipStream_t>(stream);
+    if (dtype == CHIPMUNK_DTYPE_BF16) return E == 128 ? launch_packed<Bf16, 128>(p, few, ws, ws_bytes, st) : launch_packed<Bf16, 64>(p, few, ws, ws_bytes, st);
+    return E == 128 ? launch_packed<Fp16, 128>(p, few, ws, ws_bytes, st) : launch_packed<Fp16, 64>(p, few, ws, ws_bytes, st);
 }
