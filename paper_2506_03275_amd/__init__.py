@@ -91,7 +91,7 @@ def _bind(lib):
         warnings.warn(f"the compiled binding is not used ({e}): calls take some 2 us longer (build() makes it anew)", RuntimeWarning)
         return _Python()
     names = ("voxel_reorder", "topk_cols", "attn_sparse_delta", "attn_dense", "attn_dense_colsum_stale", "mlp_tile_mean_preact",
-             "mlp_sparse_delta", "mlp_dense")
+             "mlp_sparse_delta", "mlp_dense", "linear", "rope", "attn_packed")
     _native.bind({"chipmunk_" + n: ctypes.cast(getattr(lib, "chipmunk_" + n), _c_ptr).value for n in names}, _current_device, _raw_stream)
     return _native
 
@@ -161,6 +161,10 @@ if _current_device is not None and _raw_stream is not None:
 else:
     def _stream():
         return torch.cuda.current_stream().cuda_stream
+
+
+def _device():
+    return torch.cuda.current_device() if _current_device is None else _current_device()
 
 
 def voxel_reorder(src, dst, perm, inv_perm, n_prefix, T, H, W, n_suffix, vt, vh, vw, inverse=False):
@@ -391,7 +395,7 @@ def _strided(t, dtype, name, dims):
         raise ValueError(f"{name}: must have {dims} dimensions")
     if t.device.type != "cuda":
         raise ValueError(f"{name}: must live on the GPU")
-    if t.device.index != torch.cuda.current_device():
+    if t.device.index != _device():
         raise ValueError(f"{name}: must live on the current device")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: rows must be dense")
@@ -408,6 +412,9 @@ def _element(t, name):
 def linear(x, w, bias, residual, out, act=ACT_NONE):
     """out = act(x w^T + bias) + residual.  x: [N, D], residual (or None), out: [N, F], rows dense, any row stride; w: [F, D], bias:
     [F] or None, contiguous; all bf16 or all fp16.  out may be residual."""
+    status = _fast.linear(x, w, bias, residual, out, act)
+    if status is not None:
+        return _check(status, "chipmunk_linear")
     dtype, number = _element(x, "x")
     px, pr, po = _strided(x, dtype, "x", 2), _strided(residual, dtype, "residual", 2), _strided(out, dtype, "out", 2)
     pw, pb = _strided(w, dtype, "w", 2), _strided(bias, dtype, "bias", 1)
@@ -416,13 +423,8 @@ def linear(x, w, bias, residual, out, act=ACT_NONE):
         raise ValueError("w: must be contiguous, with rows as long as x's")
     if tuple(out.shape) != (N, F) or (residual is not None and residual.shape != out.shape) or (bias is not None and bias.shape[0] != F):
         raise ValueError("out and residual must be [rows of x, rows of w], bias [rows of w]")
-    _check(load().chipmunk_linear(px, _row_stride(x), pw, pb, pr, 0 if residual is None else _row_stride(residual), po, _row_stride(out), N, D, F,
+    _check(load().chipmunk_linear(px, x.stride(0), pw, pb, pr, 0 if residual is None else residual.stride(0), po, out.stride(0), N, D, F,
                                   int(act), number, _stream()), "chipmunk_linear")
-
-
-def _row_stride(t):
-    """A single row's stride means nothing."""
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
 
 
 def rope_frequencies(axes, theta=10000.0, device="cuda"):
@@ -434,6 +436,9 @@ def rope(x, pos, freqs, out, axes, halves=False, inverse=False):
     """Rotary positions.  x, out: [tokens, heads, E] bf16 or fp16, any strides of tokens and heads (x.transpose(0, 1) of heads of
     rows); out may be x.  pos: int32 [tokens, 3]; freqs: fp64 [pairs]; axes: pairs of the three axes; halves: pair j is elements j
     and j + pairs, else 2 j and 2 j + 1; inverse: by the opposite angle, the gradient of the turn."""
+    status = _fast.rope(x, pos, freqs, out, axes, halves, inverse)
+    if status is not None:
+        return _check(status, "chipmunk_rope")
     dtype, number = _element(x, "x")
     px, po = _strided(x, dtype, "x", 3), _strided(out, dtype, "out", 3)
     pp, pf = _strided(pos, torch.int32, "pos", 2), _strided(freqs, torch.float64, "freqs", 1)
@@ -455,6 +460,9 @@ def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k
     """Attention over packed sequences.  q, out: [Tq, Hq, E], k, v: [Tk, Hk, E], bf16 or fp16, any strides of rows and heads; cu_q,
     cu_k: int32 [S + 1], where the sequences start; k_len: int32 [S] or None, keys in use from there on; max_q, max_k: no
     sequence has more queries, keys; ws: uint8 workspace of attn_packed_workspace_bytes (none needed where that is 0)."""
+    status = _fast.attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k_len, ws)
+    if status is not None:
+        return _check(status, "chipmunk_attn_packed")
     dtype, number = _element(q, "q")
     i32 = torch.int32
     pq, pk, pv, po = (_strided(t, dtype, name, 3) for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out")))
@@ -465,11 +473,7 @@ def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k
         raise ValueError("out must have the shape of q, v that of k, and all the same E")
     if cu_k.shape[0] != S + 1 or (k_len is not None and k_len.shape[0] != S):
         raise ValueError("cu_q and cu_k must be [sequences + 1], k_len [sequences]")
-    strides = [s for t in (q, k, v, out) for s in (_row_stride3(t), t.stride(1))]
+    strides = [s for t in (q, k, v, out) for s in (t.stride(0), t.stride(1))]
     _check(load().chipmunk_attn_packed(pq, strides[0], strides[1], pk, strides[2], strides[3], pv, strides[4], strides[5], po, strides[6], strides[7],
                                        pcq, pck, pkl, S, Tq, Tk, Hq, Hk, E, max_q, max_k, int(bool(causal)), float(softmax_scale), number,
                                        pws, 0 if ws is None else ws.numel(), _stream()), "chipmunk_attn_packed")
-
-
-def _row_stride3(t):
-    return t.stride(0) if t.shape[0] > 1 else t.shape[2]

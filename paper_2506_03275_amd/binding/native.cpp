@@ -20,8 +20,10 @@ struct Entry {
 Entry entries[] = {{"chipmunk_voxel_reorder", nullptr},       {"chipmunk_topk_cols", nullptr},
                    {"chipmunk_attn_sparse_delta", nullptr},   {"chipmunk_attn_dense", nullptr},
                    {"chipmunk_attn_dense_colsum_stale", nullptr}, {"chipmunk_mlp_tile_mean_preact", nullptr},
-                   {"chipmunk_mlp_sparse_delta", nullptr},    {"chipmunk_mlp_dense", nullptr}};
-enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense };
+                   {"chipmunk_mlp_sparse_delta", nullptr},    {"chipmunk_mlp_dense", nullptr},
+                   {"chipmunk_linear", nullptr},              {"chipmunk_rope", nullptr},
+                   {"chipmunk_attn_packed", nullptr}};
+enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense, kLinear, kRope, kAttnPacked };
 PyObject* current_device = nullptr;   // torch's functions that name the current device and, for a device, its current stream
 PyObject* raw_stream = nullptr;
 
@@ -270,6 +272,106 @@ PyObject* mlp_dense(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// ---- tensors with strides: one call's are on the current device, of one element type, with dense last dimensions ----
+struct Strided {
+    Args& a;
+    int device = -1;
+    at::ScalarType element = at::kBFloat16;
+
+    // the call's element type is that of argument i
+    explicit Strided(Args& args, int i) : a(args) {
+        const at::Tensor* t = a.tensor(i);
+        if (!a.ok) return;
+        element = t->scalar_type();
+        if (element != at::kBFloat16 && element != at::kHalf) a.ok = false;
+        PyObject* number = PyObject_CallNoArgs(current_device);
+        device = number ? (int)PyLong_AsLong(number) : -1;
+        Py_XDECREF(number);
+        if (PyErr_Occurred()) a.ok = false;
+    }
+    const at::Tensor* tensor(int i, int dims, at::ScalarType type) {
+        const at::Tensor* t = a.tensor(i);
+        if (!a.ok) return nullptr;
+        if (t->dim() != dims || t->scalar_type() != type || t->numel() == 0 || t->device().type() != at::kCUDA || t->device().index() != device ||
+            (t->size(dims - 1) > 1 && t->stride(dims - 1) != 1))
+            a.ok = false;
+        for (int d = 0; a.ok && d < dims; d++)
+            if (t->size(d) > INT_MAX) a.ok = false;
+        return a.ok ? t : nullptr;
+    }
+    const at::Tensor* elements(int i, int dims) { return tensor(i, dims, element); }
+    const at::Tensor* optional(int i, int dims, at::ScalarType type) { return a.ok && !a.none(i) ? tensor(i, dims, type) : nullptr; }
+    int number() const { return element == at::kBFloat16 ? 0 : 1; }
+    bool truth(int i) {
+        if (a.ok && !PyBool_Check(a.v[i])) a.ok = false;
+        return a.ok && a.v[i] == Py_True;
+    }
+};
+const uint16_t* elements_of(const at::Tensor* t) { return t ? static_cast<const uint16_t*>(t->data_ptr()) : nullptr; }
+
+// x, w, bias, residual, out, act
+PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kLinear, args, n, 6, [](Args& a, auto run) {
+        Strided s(a, 0);
+        const at::Tensor *x = s.elements(0, 2), *w = s.elements(1, 2), *bias = s.optional(2, 1, s.element), *residual = s.optional(3, 2, s.element), *out = s.elements(4, 2);
+        const int act = a.integer(5);
+        if (!a.ok || !w->is_contiguous() || w->size(1) != x->size(1) || out->size(0) != x->size(0) || out->size(1) != w->size(0) ||
+            (residual && residual->sizes() != out->sizes()) || (bias && bias->size(0) != w->size(0))) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_linear){}, elements_of(x), x->stride(0), elements_of(w), elements_of(bias), elements_of(residual), residual ? residual->stride(0) : (int64_t)0,
+            const_cast<uint16_t*>(elements_of(out)), out->stride(0), (int)x->size(0), (int)x->size(1), (int)w->size(0), act, s.number(), stream);
+    });
+}
+
+// x, pos, freqs, out, axes, halves, inverse
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kRope, args, n, 7, [](Args& a, auto run) {
+        Strided s(a, 0);
+        const at::Tensor *x = s.elements(0, 3), *pos = s.tensor(1, 2, at::kInt), *freqs = s.tensor(2, 1, at::kDouble), *out = s.elements(3, 3);
+        if (!a.ok || (!PyList_CheckExact(a.v[4]) && !PyTuple_CheckExact(a.v[4])) || PySequence_Fast_GET_SIZE(a.v[4]) != 3) {
+            a.ok = false;
+            return;
+        }
+        Args axes{PySequence_Fast_ITEMS(a.v[4]), true};
+        const int t = axes.integer(0), h = axes.integer(1), w = axes.integer(2);
+        const bool halves = s.truth(5), inverse = s.truth(6);
+        if (!a.ok || !axes.ok || out->sizes() != x->sizes() || pos->size(0) != x->size(0) || pos->size(1) != 3 || !pos->is_contiguous() ||
+            freqs->size(0) != (int64_t)t + h + w) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_rope){}, elements_of(x), x->stride(0), x->stride(1), (const int32_t*)pos->data_ptr(), (const double*)freqs->data_ptr(),
+            const_cast<uint16_t*>(elements_of(out)), out->stride(0), out->stride(1), (int)x->size(0), (int)x->size(1), (int)x->size(2), t, h, w, (int)halves, (int)inverse,
+            s.number(), stream);
+    });
+}
+
+// q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k_len, ws
+PyObject* attn_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kAttnPacked, args, n, 12, [](Args& a, auto run) {
+        Strided s(a, 0);
+        const at::Tensor *q = s.elements(0, 3), *k = s.elements(1, 3), *v = s.elements(2, 3), *cu_q = s.tensor(3, 1, at::kInt), *cu_k = s.tensor(4, 1, at::kInt),
+                         *out = s.elements(5, 3), *k_len = s.optional(10, 1, at::kInt), *ws = s.optional(11, 1, at::kByte);
+        const int max_q = a.integer(6), max_k = a.integer(7);
+        const bool causal = s.truth(8);
+        const float scale = a.real(9);
+        if (!a.ok || out->sizes() != q->sizes() || k->sizes() != v->sizes() || k->size(2) != q->size(2) || cu_k->size(0) != cu_q->size(0) ||
+            (k_len && k_len->size(0) != cu_q->size(0) - 1)) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_attn_packed){}, elements_of(q), q->stride(0), q->stride(1), elements_of(k), k->stride(0), k->stride(1), elements_of(v), v->stride(0), v->stride(1),
+            const_cast<uint16_t*>(elements_of(out)), out->stride(0), out->stride(1), (const int32_t*)cu_q->data_ptr(), (const int32_t*)cu_k->data_ptr(),
+            k_len ? (const int32_t*)k_len->data_ptr() : nullptr, (int)(cu_q->size(0) - 1), (int)q->size(0), (int)k->size(0), (int)q->size(1), (int)k->size(1), (int)q->size(2), max_q,
+            max_k, (int)causal, scale, s.number(), ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->numel() : (size_t)0, stream);
+    });
+}
+
 // bind(addresses: dict of names, current_device, raw_stream)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 3 || !PyDict_Check(args[0])) {
@@ -291,6 +393,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(voxel_reorder), FAST(topk_cols), FAST(attn_sparse_delta), FAST(attn_dense),
                          FAST(attn_dense_colsum_stale), FAST(mlp_tile_mean_preact), FAST(mlp_sparse_delta), FAST(mlp_dense),
+                         FAST(linear), FAST(rope), FAST(attn_packed),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

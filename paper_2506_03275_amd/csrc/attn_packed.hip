@@ -823,6 +823,8 @@ extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_strid
     if (!is_positive_finite_scalar(softmax_scale)) return CHIPMUNK_ERR_SHAPE;
     if ((E != 64 && E != 128) || (dtype != CHIPMUNK_DTYPE_BF16 && dtype != CHIPMUNK_DTYPE_FP16)) return CHIPMUNK_ERR_UNSUPPORTED;
     constexpr int64_t kMostStride = 1 << 24;
+    if (Tq == 1) q_token_stride = out_token_stride = E;   // of one row alone a stride means nothing
+    if (Tk == 1) k_token_stride = v_token_stride = E;
     for (int64_t token : {q_token_stride, k_token_stride, v_token_stride, out_token_stride})
         if (token < E || token >= kMostStride) return CHIPMUNK_ERR_SHAPE;
     if ((Hq > 1 && (q_head_stride < E || out_head_stride < E)) || (Hk > 1 && (k_head_stride < E || v_head_stride < E))) return CHIPMUNK_ERR_SHAPE;

@@ -765,6 +765,10 @@ extern "C" int32_t chipmunk_linear(const uint16_t* x, int64_t ldx, const uint16_
                                    uint16_t* out, int64_t ldo, int N, int D, int F, int act, int dtype, void* stream) {
     if (!x || !w || !out) return CHIPMUNK_ERR_NULL;
     constexpr int64_t kMostStride = 1 << 22;
+    if (N == 1) {                                             // of one row alone a stride means nothing
+        ldx = D;
+        ldo = ldr = F;
+    }
     if (N <= 0 || D <= 0 || F <= 0 || D >= 1 << 20) return CHIPMUNK_ERR_SHAPE;
     if (ldx < D || ldo < F || (residual && ldr < F) || ldx >= kMostStride || ldo >= kMostStride || (residual && ldr >= kMostStride)) return CHIPMUNK_ERR_SHAPE;
     if (D % 8 != 0 || F % 8 != 0 || act < CHIPMUNK_ACT_GELU_ERF || act > CHIPMUNK_ACT_SILU || (dtype != CHIPMUNK_DTYPE_BF16 && dtype != CHIPMUNK_DTYPE_FP16))

@@ -106,6 +106,8 @@ extern "C" int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int6
         return !((tokens == 1 || token >= (__int128)(heads - 1) * head + E) && (heads == 1 || head >= E)) &&
                !((heads == 1 || head >= (__int128)(tokens - 1) * token + E) && (tokens == 1 || token >= E));
     };
+    if (tokens == 1) x_token_stride = out_token_stride = 0;   // of one row alone a stride means nothing
+    if (heads == 1) x_head_stride = out_head_stride = 0;
     if (overlap(x_token_stride, x_head_stride) || overlap(out_token_stride, out_head_stride)) return CHIPMUNK_ERR_SHAPE;
     if (!aligned16(x) || !aligned16(out) || (reinterpret_cast<uintptr_t>(pos) & 3) || (reinterpret_cast<uintptr_t>(freqs) & 7) ||
         (x_token_stride | x_head_stride | out_token_stride | out_head_stride) % 8 != 0)
