@@ -3,13 +3,15 @@
 // where the first pairs belong to axis 0 (time), the next to axis 1 (height), the last to axis 2 (width).  The inverse, by the
 // opposite angle, is the gradient of the turn.
 //
-// Bound: memory, 2 E bytes read and 2 E written per row of a head.  An angle belongs to a token and a pair and serves every head,
+// Bound: memory, 2 E bytes read and 2 E written per row of a head: 4608 tokens x 48 heads x 128 take 21 us (5.3 TB/s), 18 000 x 80 131 us
+// (5.6 TB/s; a large copy reaches 5.2 to 5.8).  An angle belongs to a token and a pair and serves every head,
 // so a thread keeps the sines of its four (or eight) pairs and walks heads.  An angle is formed in 64 bits: positions go to 2^31, and
 // in 32 bits the angle of position 100 000 is off by 4e-3.  What is left of it after the whole turns, rounded to 32 bits, goes to
 // the sine and cosine instructions, which take turns.
 #include "element.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace chipmunk {
 
@@ -30,9 +32,14 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeAhead = 4;    // heads of a thread in flight
 constexpr int kRopeMostHeads = 1 << 16;
 
+// A source beyond the L2s passes them by, and a result beyond the last-level cache passes that by as well.  Measured with the kernel that reads
+// the result: 113 MB 43.9 us, sources past 38.6, results too 43.3; 737 MB 267, 262, 253; 28 MB 19.3, 21.4, 23.5.
+constexpr int64_t kRopeL2 = 32 << 20, kRopeLastLevel = 256 << 20;
+enum RopePast { kNothing = 0, kSource = 1, kSourceAndResult = 2 };
+
 // A thread's item of a row: ADJACENT pairs (elements 2j, 2j + 1), eight elements that hold four pairs; HALVES (elements j, j +
 // pairs), the eight elements of eight pairs in either half.  Items behind the pairs are copied.
-template <class T, bool HALVES>
+template <class T, bool HALVES, int PAST>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     constexpr int NP = HALVES ? 8 : 4;
     const int slot = threadIdx.x / p.items, item = threadIdx.x - slot * p.items;
@@ -41,6 +48,15 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     const int turned = p.pairs / NP;                     // items that hold pairs
     const bool turn = item < turned;
     const int64_t e0 = HALVES && !turn ? 2 * p.pairs + (item - turned) * 8 : item * 8, e1 = HALVES && turn ? e0 + p.pairs : e0;
+    auto load = [](const uint16_t* at) {
+        const u32x4* words = reinterpret_cast<const u32x4*>(at);
+        return PAST >= kSource ? __builtin_nontemporal_load(words) : *words;
+    };
+    auto store = [](uint16_t* at, u32x4 value) {
+        u32x4* words = reinterpret_cast<u32x4*>(at);
+        if (PAST == kSourceAndResult) __builtin_nontemporal_store(value, words);
+        else *words = value;
+    };
     const int last_head = min(p.heads, ((int)blockIdx.y + 1) * p.side * p.per);
     for (int64_t t = (int64_t)blockIdx.x * p.at_once + in_group; t < p.tokens; t += (int64_t)gridDim.x * p.at_once) {
         float c[NP], s[NP];
@@ -62,8 +78,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
 #pragma unroll
             for (int n = 0; n < kRopeAhead; n++) {
                 const int64_t row = (int64_t)min(h + n * p.side, last_head - 1) * p.x_head;
-                a[n] = *reinterpret_cast<const u32x4*>(from + row + e0);
-                if (HALVES) b[n] = *reinterpret_cast<const u32x4*>(from + row + e1);
+                a[n] = load(from + row + e0);
+                if (HALVES) b[n] = load(from + row + e1);
             }
 #pragma unroll
             for (int n = 0; n < kRopeAhead; n++) {
@@ -82,11 +98,23 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
                     }
                 }
                 const int64_t row = (int64_t)(h + n * p.side) * p.out_head;
-                *reinterpret_cast<u32x4*>(to + row + e0) = a[n];
-                if (HALVES && turn) *reinterpret_cast<u32x4*>(to + row + e1) = b[n];
+                store(to + row + e0, a[n]);
+                if (HALVES && turn) store(to + row + e1, b[n]);
             }
         }
     }
+}
+
+template <class T>
+static void rope_launch(const RopeParams& p, dim3 grid, bool halves, int past, hipStream_t s) {
+    auto go = [&](auto halves_c) {
+        constexpr bool HALVES = decltype(halves_c)::value;
+        if (past == kNothing) rope_kernel<T, HALVES, kNothing><<<grid, kRopeThreads, 0, s>>>(p);
+        else if (past == kSource) rope_kernel<T, HALVES, kSource><<<grid, kRopeThreads, 0, s>>>(p);
+        else rope_kernel<T, HALVES, kSourceAndResult><<<grid, kRopeThreads, 0, s>>>(p);
+    };
+    if (halves) go(std::true_type{});
+    else go(std::false_type{});
 }
 
 }  // namespace chipmunk
@@ -117,18 +145,17 @@ extern "C" int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int6
     p.items = halves ? (int)(pairs / 8 + (E - 2 * pairs) / 8) : E / 8;
     const int slots = kRopeThreads / p.items;
     p.per = kRopeAhead;
-    p.side = std::min(slots, (heads + p.per - 1) / p.per);
+    // Side by side stand heads, whose rows lie behind one another; heads of rows get four tokens' rows in one run (18 000 x 80 heads
+    // 144 -> 131 us, 75 600: 636 -> 568)
+    p.side = std::min(out_head_stride > out_token_stride ? std::min(4, slots) : slots, (heads + p.per - 1) / p.per);
     p.at_once = slots / p.side;
     const int64_t groups = ((int64_t)tokens + p.at_once - 1) / p.at_once;
     const int parts = (heads + p.side * p.per - 1) / (p.side * p.per);
     const dim3 grid((uint32_t)std::min<int64_t>(groups, (1 << 22) / parts), parts);   // a launch has fewer than 2^32 threads
     const auto s = static_cast<hipStream_t>(stream);
-    if (dtype == CHIPMUNK_DTYPE_BF16) {
-        if (halves) rope_kernel<Bf16, true><<<grid, kRopeThreads, 0, s>>>(p);
-        else rope_kernel<Bf16, false><<<grid, kRopeThreads, 0, s>>>(p);
-    } else {
-        if (halves) rope_kernel<Fp16, true><<<grid, kRopeThreads, 0, s>>>(p);
-        else rope_kernel<Fp16, false><<<grid, kRopeThreads, 0, s>>>(p);
-    }
+    const int64_t bytes = (int64_t)tokens * heads * E * 2;
+    const int past = bytes > kRopeLastLevel ? kSourceAndResult : bytes > kRopeL2 ? kSource : kNothing;
+    if (dtype == CHIPMUNK_DTYPE_BF16) rope_launch<Bf16>(p, grid, halves != 0, past, s);
+    else rope_launch<Fp16>(p, grid, halves != 0, past, s);
     return launch_status();
 }

@@ -236,7 +236,7 @@ def _positions(n, seed, most):
 
 ROPES = [(1, 1, 64, (32, 0, 0)), (1, 40, 128, (64, 0, 0)), (8, 40, 128, (64, 0, 0)), (5, 3, 64, (8, 8, 16)), (333, 7, 128, (16, 24, 24)), (77, 24, 128, (8, 28, 28)),
          (1000, 48, 128, (22, 21, 21)), (64, 5, 256, (40, 44, 44)), (100, 2, 80, (0, 16, 16)), (33, 65, 8, (4, 0, 0)), (17, 9, 512, (128, 64, 64)),
-         (200, 100, 96, (16, 0, 16)), (3, 1000, 64, (8, 12, 12))]
+         (200, 100, 96, (16, 0, 16)), (3, 1000, 64, (8, 12, 12)), (2100, 70, 128, (16, 24, 24)), (20011, 53, 128, (22, 21, 21))]   # the last two past the L2s, past every cache
 
 
 @gpu
