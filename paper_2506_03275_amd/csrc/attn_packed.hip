@@ -90,12 +90,16 @@ __device__ __forceinline__ bool find_tile(const PackedParams& p, int tile, int l
 template <int NQB>
 __device__ __forceinline__ void hide_keys(f32x4 (&S)[2][NQB], int first, const int (&limit)[NQB]) {
 #pragma unroll
-    for (int u = 0; u < 2; u++)
+    for (int qb = 0; qb < NQB; qb++) {
+        const int left = limit[qb] - first;
 #pragma unroll
-        for (int r = 0; r < 4; r++)
+        for (int u = 0; u < 2; u++)
 #pragma unroll
-            for (int qb = 0; qb < NQB; qb++)
-                if (first + u * 16 + r >= limit[qb]) S[u][qb][r] = -INFINITY;
+            for (int r = 0; r < 4; r++) {
+                S[u][qb][r] = u * 16 + r < left ? S[u][qb][r] : -INFINITY;
+                asm volatile("" : "+v"(S[u][qb][r]));   // one behind the other: all comparisons' masks at a time do not fit the scalar registers
+            }
+    }
 }
 
 template <class T, int E, int NQB>
@@ -163,19 +167,17 @@ __device__ __forceinline__ void tile_scores(f32x4 (&S)[2][NQB], const RowState<T
     }
 }
 
-// Whether the lower or the upper element of a word is infinite or NaN.  (On the bits: these files are compiled as if NaN did not
-// exist, and a comparison of values is folded accordingly.)
+// The top bit of either element of a word that is infinite or NaN: one more in the last place of an exponent of all ones carries into it.
+// (On the bits: these files are compiled as if NaN did not exist, and a comparison of values is folded accordingly.)
 template <class T>
-__device__ __forceinline__ bool low_not_finite(uint32_t word) { return (~word & T::kExponent & 0xffffu) == 0; }
-template <class T>
-__device__ __forceinline__ bool high_not_finite(uint32_t word) { return (~word & T::kExponent & 0xffff0000u) == 0; }
+__device__ __forceinline__ uint32_t not_finite(uint32_t word) { return ((word & T::kExponent) + T::kExponentStep) & 0x80008000u; }
 
 // One word of two elements without those that are infinite or NaN; they are noted in `found`.
 template <class T>
-__device__ __forceinline__ uint32_t finite_elements(uint32_t word, bool& found) {
-    const bool low = low_not_finite<T>(word), high = high_not_finite<T>(word);
-    found |= low || high;
-    return word & ((low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u));
+__device__ __forceinline__ uint32_t finite_elements(uint32_t word, uint32_t& found) {
+    const uint32_t tops = not_finite<T>(word);
+    found |= tops;
+    return word & ~((tops - (tops >> 15)) | tops);
 }
 
 // P = exp2(S sl2) rounded to the element type (to 8 or 11 bits, like the values that it weights), its sum, and O^T += V^T P^T.
@@ -183,7 +185,7 @@ __device__ __forceinline__ uint32_t finite_elements(uint32_t word, bool& found) 
 // be a NaN: such values are left out and noted.
 template <class T, int E, int NQB, bool HIDDEN>
 __device__ __forceinline__ void tile_values(RowState<T, E, NQB>& st, const f32x4 (&S)[2][NQB], const uint32_t (&vaddr)[E / 16], int tile_off, float sl2,
-                                            bool& found) {
+                                            uint32_t& found) {
     typedef typename T::x8 x8;
     typedef __attribute__((ext_vector_type(8))) short short8v;
     constexpr int ROWB = E * 2, NEB = E / 16, AHEAD = 2;
@@ -239,7 +241,7 @@ __device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, cons
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 float value = r % 2 ? T::high(words[r / 2]) : T::low(words[r / 2]);
-                const bool special = r % 2 ? high_not_finite<T>(words[r / 2]) : low_not_finite<T>(words[r / 2]);
+                const bool special = not_finite<T>(words[r / 2]) & (r % 2 ? 0x80000000u : 0x8000u);
                 asm volatile("" : "+v"(value));           // nothing is known of it, not even that it is none of the two
 #pragma unroll
                 for (int qb = 0; qb < NQB; qb++)
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void attn_packed_rows_kernel(PackedParams p
     };
     // The steps whose keys all of the wave's rows see, in two copies, whose LDS offsets are constants; then those with hidden keys.
     // Waves may stand in different loops: each step of each is one barrier.
-    bool found = false;
+    uint32_t found = 0;
     auto step = [&](auto half_c, int first) {
         constexpr int half = decltype(half_c)::value;
         arrived(first);
@@ -401,31 +403,35 @@ __global__ __launch_bounds__(256, 2) void attn_packed_rows_kernel(PackedParams p
         first += kStepKeys;
     }
     const int first_hidden = first;
+    int half = first / kStepKeys & 1;
+    auto move = [&](int bytes) {                          // the addresses to the other half
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
+    };
+    move(half * kStepTiles * STAGE);
 #pragma unroll 1
-    for (; first < keys; first += kStepKeys) {
-        const int half = first / kStepKeys & 1;
+    for (; first < keys; first += kStepKeys, half ^= 1) {
         arrived(first);
 #pragma unroll
         for (int j = 0; j < E / 16; j++) request(half ^ 1, j);
-        if (first >= seen) continue;                      // nothing to see for this wave
-        uint32_t kat[E / 32], vat[E / 16];
+        if (first < seen) {                               // else nothing to see for this wave
 #pragma unroll
-        for (int es = 0; es < E / 32; es++) kat[es] = kaddr[es] + half * kStepTiles * STAGE;
-#pragma unroll
-        for (int eb = 0; eb < E / 16; eb++) vat[eb] = vaddr[eb] + half * kStepTiles * STAGE;
-#pragma unroll
-        for (int n = 0; n < kStepTiles; n++) {
-            f32x4 S[2][NQB];
-            tile_scores<T, E, NQB>(S, st, kat, n * STAGE, [](int) {});
-            hide_keys<NQB>(S, first + n * kTile + 4 * g, limit);
-            raise_reference<T, E, NQB>(st, S, p.sl2, slack);
-            tile_values<T, E, NQB, true>(st, S, vat, n * STAGE + TILE, p.sl2, found);
+            for (int n = 0; n < kStepTiles; n++) {
+                f32x4 S[2][NQB];
+                tile_scores<T, E, NQB>(S, st, kaddr, n * STAGE, [](int) {});
+                hide_keys<NQB>(S, first + n * kTile + 4 * g, limit);
+                raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+                tile_values<T, E, NQB, true>(st, S, vaddr, n * STAGE + TILE, p.sl2, found);
+            }
         }
+        move(half ? -kStepTiles * STAGE : kStepTiles * STAGE);
     }
     wait_all_memory();                                    // the transfers behind the last step
 
     // Infinite and NaN values among the steps with hidden keys go to the queries that see them.
-    if (__builtin_amdgcn_ballot_w64(found) != 0) add_special_values<T, E, NQB>(st, vh, p.v_token, first_hidden, seen, limit, g);
+    if (__builtin_amdgcn_ballot_w64(found != 0) != 0) add_special_values<T, E, NQB>(st, vh, p.v_token, first_hidden, seen, limit, g);
 
 #pragma unroll
     for (int qb = 0; qb < NQB; qb++) {
@@ -530,7 +536,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
         request(kh, p.k_token, from_k, first, lds0);
         request(vh, p.v_token, from_v, first, lds0 + TILE);
     }
-    bool found = false;
+    uint32_t found = 0;
     auto tile = [&](auto hidden_c) {
         constexpr bool HIDDEN = decltype(hidden_c)::value;
         f32x4 S[2][NQB];
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
 #pragma unroll 1
     for (; first < end; first += TURN) tile(std::true_type{});
     wait_all_memory();
-    if (__builtin_amdgcn_ballot_w64(found) != 0)
+    if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
         for (int at = first_hidden; at < end; at += TURN) add_special_values<T, E, NQB>(st, vh, p.v_token, at, min(end, at + kTile), limit, g);
     lds_accesses_then_barrier();                          // every wave is done with its tiles
 

@@ -12,7 +12,7 @@ typedef __attribute__((ext_vector_type(2))) _Float16 fp16x2;
 // 0..15; low, high: the two elements of a word
 struct Bf16 {
     typedef bf16x8 x8;
-    static constexpr uint32_t kOnes = 0x3f803f80u, kExponent = 0x7f807f80u;
+    static constexpr uint32_t kOnes = 0x3f803f80u, kExponent = 0x7f807f80u, kExponentStep = 0x00800080u;
     static __device__ __forceinline__ f32x4 product(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x16 product(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
@@ -21,7 +21,7 @@ struct Bf16 {
 };
 struct Fp16 {
     typedef fp16x8 x8;
-    static constexpr uint32_t kOnes = 0x3c003c00u, kExponent = 0x7c007c00u;
+    static constexpr uint32_t kOnes = 0x3c003c00u, kExponent = 0x7c007c00u, kExponentStep = 0x04000400u;
     static __device__ __forceinline__ f32x4 product(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x16 product(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return __builtin_bit_cast(uint32_t, fp16x2{(_Float16)lo, (_Float16)hi}); }
