@@ -11,14 +11,17 @@ With `overlap`, the index computation of the NEXT block (scores GEMM + top-k, wh
 and weights) runs on a second stream beside the current block's attention and MLP delta; an event hands the indices
 over.  In a real DiT the next block's input depends on this block's output, so that overlap is a property of a stack
 with pre-generated inputs; what carries over to a model is that the index work needs no result of the delta kernels.
+
+AttentionLayer is the attention half of a block with its projections, for sequences packed one behind the other: a text
+encoder over prompts of different lengths, images of different sizes, or single tokens over what their caches hold.
 """
 import math
 
 import torch
 
 from . import (ACT_GELU_TANH, attn_dense, attn_dense_colsum_stale, attn_dense_row_stats,
-               attn_dense_workspace_bytes, attn_sparse_delta, mlp_dense,
-               mlp_sparse_delta, mlp_tile_mean_preact, mlp_tile_mean_workspace_bytes, mlp_workspace_bytes,
+               attn_dense_workspace_bytes, attn_packed, attn_packed_workspace_bytes, attn_sparse_delta, linear, mlp_dense,
+               mlp_sparse_delta, mlp_tile_mean_preact, mlp_tile_mean_workspace_bytes, mlp_workspace_bytes, rope,
                topk_cols)
 
 
@@ -133,3 +136,49 @@ def sparse_step(blocks, step, side_stream=None, after_block=None):
         if after_block:
             after_block(b, blk)
     main.wait_stream(side_stream)
+
+
+class AttentionLayer:
+    """x + W_out attention(rope(W_qkv x)) over packed sequences, whose keys and values are kept in caches.
+
+    w_qkv: [(heads + 2 kv_heads) E, D], rows of queries, keys, values; w_out: [D, heads E]; biases [..] or None; freqs: fp64,
+    and axes, halves: as rope takes them.  A sequence has a slot of `slot_tokens` rows in the caches; step() appends its
+    tokens there and attends to all that the slot then holds.
+    """
+
+    def __init__(self, w_qkv, b_qkv, w_out, b_out, heads, kv_heads, freqs, axes, slots, slot_tokens, causal=True, halves=False):
+        self.w_qkv, self.b_qkv, self.w_out, self.b_out, self.freqs, self.axes = w_qkv, b_qkv, w_out, b_out, freqs, axes
+        self.heads, self.kv_heads, self.causal, self.halves = heads, kv_heads, causal, halves
+        self.E = w_qkv.shape[0] // (heads + 2 * kv_heads)
+        self.scale = 1.0 / math.sqrt(self.E)
+        dev, dtype = w_qkv.device, w_qkv.dtype
+        self.slot_tokens = slot_tokens
+        self.k_cache = torch.empty((slots * slot_tokens, kv_heads, self.E), dtype=dtype, device=dev)
+        self.v_cache = torch.empty_like(self.k_cache)
+        self.starts = torch.arange(slots + 1, dtype=torch.int32, device=dev) * slot_tokens
+
+    def buffers(self, tokens, max_q, max_k):
+        """What a step over so many tokens works in: projections, attention and result, and the workspace.  Two steps that may
+        overlap, also as captured graphs, need buffers of their own."""
+        like = dict(dtype=self.w_qkv.dtype, device=self.w_qkv.device)
+        slots = self.starts.shape[0] - 1
+        return dict(qkv=torch.empty((tokens, self.heads + 2 * self.kv_heads, self.E), **like),
+                    att=torch.empty((tokens, self.heads, self.E), **like), out=torch.empty((tokens, self.w_out.shape[0]), **like),
+                    max_q=max_q, max_k=max_k,
+                    ws=_u8(attn_packed_workspace_bytes(slots, self.heads, self.kv_heads, self.E, max_q, max_k), self.w_qkv.device))
+
+    def step(self, x, pos, cu_q, rows, k_len, buffers):
+        """x: [tokens, D], the slots' sequences one behind the other (cu_q int32 [slots + 1], a slot without new tokens has
+        none); pos: int32 [tokens, 3]; rows: int64 [tokens], each token's row of the caches (slot * slot_tokens + its place);
+        k_len: int32 [slots], tokens of each slot, the new ones among them.  Returns buffers["out"]."""
+        b, H, Hk = buffers, self.heads, self.kv_heads
+        qkv = b["qkv"]
+        linear(x, self.w_qkv, self.b_qkv, None, qkv.view(qkv.shape[0], -1))
+        turned = qkv[:, :H + Hk]
+        rope(turned, pos, self.freqs, turned, self.axes, halves=self.halves)
+        self.k_cache.index_copy_(0, rows, qkv[:, H:H + Hk])
+        self.v_cache.index_copy_(0, rows, qkv[:, H + Hk:])
+        attn_packed(qkv[:, :H], self.k_cache, self.v_cache, cu_q, self.starts, b["att"], b["max_q"], b["max_k"], self.causal, self.scale,
+                    k_len=k_len, ws=b["ws"])
+        linear(b["att"].view(b["att"].shape[0], -1), self.w_out, self.b_out, x, b["out"])
+        return b["out"]
