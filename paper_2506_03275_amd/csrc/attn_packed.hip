@@ -468,11 +468,13 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, l16 = lane & 15;
-    // workgroups go to the XCDs in turn: a sequence's heads, whose rows lie side by side, to all of them
+    // Workgroups go to the XCDs in turn, and an XCD's to its groups of CUs: a sequence's heads, whose rows lie side by side, to all XCDs; then its
+    // parts and rows, the last ones, which may see the most, first; then the next sequence.  (Sequences side by side give every fourth workgroup
+    // of an XCD to the longest of four, which one group of CUs then walks: 1179 and three of 201 tokens, 8 heads 28.7 us.)
     int id = (int)(blockIdx.x / p.Hk);
-    const int head = (int)blockIdx.x % p.Hk, s = id % p.S;
-    id /= p.S;
-    const int part = id % p.parts, row0 = (p.tiles - 1 - id / p.parts) * 16 * NQB;   // the last rows, which may see the most, first
+    const int head = (int)blockIdx.x % p.Hk, part = id % p.parts;
+    id /= p.parts;
+    const int row0 = (p.tiles - 1 - id % p.tiles) * 16 * NQB, s = id / p.tiles;
     const Rows qs = queries_of(p, s), ks = keys_of(p, s);
     const int rows = min(16 * NQB, qs.count * p.G - row0);
     if (rows <= 0) return;
@@ -729,17 +731,17 @@ static size_t few_bytes(const FewPlan& f, int S, int Hk, int E) {
 
 // Everything else has a form by its price in us: how many workgroups there are, each with its start and end, 512 of them side by side; what
 // 64 keys take the workgroup that has the most of them, which bounds a small launch; what 64 rows x 64 keys take where the CUs are full, and a share
-// of the last workgroup.  Fitted to 2321 random batches of 1 to 32 sequences of up to 10 000 tokens, 1 to 120 heads, causal or not: the form
-// taken is 1.016 times the quickest's time in the mean.  The lengths are on the device: one sequence of the given limits is assumed, and the
+// of the last workgroup.  Fitted to 2567 random batches of 1 to 32 sequences of up to 10 000 tokens, 1 to 120 heads, causal or not: the form
+// taken is 1.010 times the quickest's time in the mean.  The lengths are on the device: one sequence of the given limits is assumed, and the
 // rest of the rows evenly spread over the others.
 enum PackedForm { kKeys16, kKeys32, kRows64, kRows128, kRows192, kPackedForms };
 struct PackedPrice {
     int rows;
     float start, alone, full;
 };
-static const PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.3f, 0.27f, 0.76f}, {32, 4.4f, 0.27f, 0.43f}, {64, 2.9f, 0.64f, 0.35f}, {128, 4.1f, 1.29f, 0.30f}, {192, 8.5f, 1.14f, 0.31f}},
-                                                           {{16, 4.8f, 0.31f, 1.89f}, {32, 6.9f, 0.45f, 0.87f}, {64, 4.8f, 0.64f, 0.77f}, {128, 4.8f, 1.71f, 0.47f}, {192, 10.7f, 2.11f, 0.41f}}};
-static const float kPackedLast[2][2] = {{0.61f, 0.28f}, {0.50f, 0.45f}};   // of E = 64, 128; all keys, causal
+static const PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.8f, 0.17f, 0.81f}, {32, 6.6f, 0.21f, 0.37f}, {64, 3.2f, 0.80f, 0.36f}, {128, 4.4f, 1.26f, 0.29f}, {192, 9.2f, 1.22f, 0.275f}},
+                                                           {{16, 5.5f, 0.165f, 1.78f}, {32, 8.3f, 0.43f, 0.70f}, {64, 5.1f, 0.94f, 0.64f}, {128, 5.1f, 1.49f, 0.50f}, {192, 13.8f, 2.34f, 0.41f}}};
+static const float kPackedLast[2][2] = {{0.35f, 0.25f}, {0.49f, 0.53f}};   // of E = 64, 128; all keys, causal
 static double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
     const PackedPrice& f = kPackedPrices[E == 128][form];
     const bool grouped = form <= kKeys32;                 // rows of a key head, of all its queries' heads
