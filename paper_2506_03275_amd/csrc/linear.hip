@@ -581,22 +581,24 @@ __global__ __launch_bounds__(512, 2) void linear_wide_kernel(LinearParams p) {
     });
 }
 
-// Few rows (8 NX at most): a workgroup owns 16 CB columns of all of them, and its waves divide the contraction, in steps of 64
-// dealt out in turn.  Each wave has a ring of its own, so none waits for another before their sums meet in LDS.
+// Tiles of 16 CB columns x 8 NX rows, whose contraction the waves of a workgroup divide, in steps of 64 dealt out in turn.  Each wave has a
+// ring of its own, so none waits for another before their sums meet in LDS.
 //
 // Bound: memory, the weights read once.  They pass through LDS because a transfer then fetches whole lines of 128 bytes (eight
 // rows); straight to registers in the product's layout a load fetches 64 bytes of sixteen rows, and a CU got half the rate.
 template <class T, int CB, int NX, int STAGES>
-__global__ __launch_bounds__(512) void linear_few_rows_kernel(LinearParams p) {
+__global__ __launch_bounds__(512) void linear_patch_kernel(LinearParams p) {
     typedef typename T::x8 x8;
     constexpr int QB = (NX + 1) / 2, NT = 2 * CB + NX, STAGE = NT * 1024;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, l16 = lane & 15;
-    const int col0 = (int)blockIdx.x * 16 * CB;
+    int tp, tq;
+    if (!linear_tile(p.tiles_p, p.tiles_q, &tp, &tq)) return;
+    const int col0 = tp * 16 * CB, row0 = tq * 8 * NX;
     const i32x4 wbuf = operand_rows(p.w, p.D, col0, min(16 * CB, p.F - col0), p.D);
-    const i32x4 xbuf = operand_rows(p.x, p.ldx, 0, p.N, p.D);
+    const i32x4 xbuf = operand_rows(p.x, p.ldx, row0, min(8 * NX, p.N - row0), p.D);
     const int all_chunks = p.D / 8, steps = ((p.D + 63) / 64 - w + waves - 1) / waves;   // the wave's: w, w + waves, ...
     uint32_t off[NT];
     int chunk[NT];
@@ -654,7 +656,7 @@ __global__ __launch_bounds__(512) void linear_few_rows_kernel(LinearParams p) {
         for (int v = 0; v < waves; v++)
 #pragma unroll
             for (int a = 0; a < CB; a++) total[a][0] += sums[((v * CB + a) * QB + c) * 64 + lane];
-        linear_store<T, CB, 1>(p, total, col0, c * 16, g, l16);
+        linear_store<T, CB, 1>(p, total, col0, row0 + c * 16, g, l16);
     }
 }
 
@@ -691,37 +693,40 @@ static int32_t launch_wide(LinearParams p, hipStream_t stream) {
 }
 
 template <class T, int CB, int NX, int STAGES>
-static int32_t launch_few_rows(LinearParams p, int waves, hipStream_t stream) {
+static int32_t launch_patch(LinearParams p, int waves, hipStream_t stream) {
     const int lds = (waves * STAGES * (2 * CB + NX) + NX % 2) * 1024;   // (the sums take less; an odd number of rows is read with what lies behind)
-    const auto kernel = linear_few_rows_kernel<T, CB, NX, STAGES>;
+    const auto kernel = linear_patch_kernel<T, CB, NX, STAGES>;
     if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
-    kernel<<<(p.F + 16 * CB - 1) / (16 * CB), 64 * waves, lds, stream>>>(p);
+    kernel<<<grid_of(p, 16 * CB, 8 * NX), 64 * waves, lds, stream>>>(p);
     return launch_status();
 }
 
 // The forms of tiles.  A launch is priced in us as rounds of as many tiles as the CUs hold: each round has its start and end, and
-// for every contraction step what it takes alone and what the tiles beside it add.  Measured per form on launches of 1 to 18 000
-// rows and contractions of 256 to 8192, of one tile and of whole rounds; the last, partly filled round counts by its share.
-enum Form { kSmall, kSmallTeams, kMiddleTeams, kTwoPerCu, kBlock, kTallBlock, kWide, kForms, kFewRows = kForms };
+// for every contraction step what it takes alone and what the tiles beside it add; the last, partly filled round counts by its
+// share.  Measured per form on launches of 1 to 18 000 rows and contractions of 256 to 8192; on 1982 random ones of 17 to 1500 rows
+// and 256 to 20 000 columns the form taken is 1.014 times the quickest's time in the mean, 1.28 at most.  The small forms whose
+// waves divide the contraction are for few tiles: 190 rows, 4992 -> 520: 8.3 us by 16 x 32, 16.2 by the quickest other; 4032 -> 464
+// with 21 rows 4.7 and 12.9; 236 rows, 5440 -> 3480 29.4 and 20.4.
+enum Form { kSmall, kSmallTeams, kMiddleTeams, kTwoPerCu, kBlock, kTallBlock, kWide, kPatch16, kPatch16x32, kPatch32, kPatch64x32, kForms, kFewRows = kForms };
 struct FormPrice {
-    int columns, rows, per_round;
+    int columns, rows, per_round, parts;                  // parts: of the contraction, a wave's each
     float round, step, beside;
 };
-static const FormPrice kFormPrices[kForms] = {{64, 64, 512, 1.3f, 0.24f, 0.20f},  {64, 64, 256, 1.9f, 0.165f, 0.06f}, {64, 128, 256, 2.4f, 0.25f, 0.07f},
-                                              {128, 128, 512, 3.0f, 0.56f, 0.45f}, {128, 128, 256, 2.8f, 0.36f, 0.20f}, {128, 192, 256, 3.4f, 0.48f, 0.29f},
-                                              {256, 256, 256, 6.0f, 1.00f, 0.45f}};
+static const FormPrice kFormPrices[kForms] = {{64, 64, 512, 1, 1.5f, 0.24f, 0.20f},   {64, 64, 256, 1, 2.3f, 0.165f, 0.06f}, {64, 128, 256, 1, 2.4f, 0.25f, 0.07f},
+                                              {128, 128, 512, 1, 3.0f, 0.56f, 0.45f}, {128, 128, 256, 1, 2.8f, 0.36f, 0.20f}, {128, 192, 256, 1, 3.4f, 0.48f, 0.29f},
+                                              {256, 256, 256, 1, 6.0f, 1.00f, 0.45f}, {16, 16, 256, 8, 2.05f, 0.37f, 0.0f},   {16, 32, 256, 8, 2.18f, 0.47f, 0.05f},
+                                              {32, 32, 256, 4, 2.55f, 0.32f, 0.09f},  {64, 32, 256, 4, 3.05f, 0.50f, 0.18f}};
 static double price_of(Form form, int64_t N, int64_t D, int64_t F) {
     const FormPrice& f = kFormPrices[form];
-    const int64_t tiles = (N + f.rows - 1) / f.rows * ((F + f.columns - 1) / f.columns), steps = (D + 63) / 64;
+    const int64_t tiles = (N + f.rows - 1) / f.rows * ((F + f.columns - 1) / f.columns), steps = ((D + 63) / 64 + f.parts - 1) / f.parts;
     const int64_t whole = tiles / f.per_round, rest = tiles % f.per_round;
     return whole * (f.round + steps * (double)(f.step + f.beside)) + (rest ? f.round + steps * (f.step + f.beside * (double)rest / f.per_round) : 0.0);
 }
 
-// Few rows have a kernel that fetches the weights at the memory's rate whatever their shape (4096 x 4096, one row: 7.4 us, tiles
-// 13.5); between 17 and 32 rows only as long as its columns, 16 to a workgroup, are not many (32 rows: 4096 columns 9.6 and 13.7 us,
-// 10 880 20.4 and 18.8).
+// Up to 16 rows there is nothing to choose: a patch of all rows reads the weights once, at the memory's rate (4096 x 4096, one row:
+// 7.4 us, tiles 13.5).
 static Form linear_form(int N, int D, int F) {
-    if (N <= 16 || (N <= 32 && F <= 8192)) return kFewRows;
+    if (N <= 16) return kFewRows;
     Form best = kSmall;
     for (int f = 1; f < kForms; f++)
         if (price_of((Form)f, N, D, F) < price_of(best, N, D, F)) best = (Form)f;
@@ -737,9 +742,8 @@ static int32_t linear_launch(const LinearParams& p, hipStream_t stream) {
         const int steps = (p.D + 63) / 64;
         const bool narrow = p.F <= 12288;
         const int waves = p.F <= 4096 && steps >= 16 ? 8 : steps >= 32 ? 4 : 2;
-        if (p.N <= 8) return narrow ? launch_few_rows<T, 1, 1, 4>(p, waves, stream) : launch_few_rows<T, 2, 1, 3>(p, waves, stream);
-        if (p.N <= 16) return narrow ? launch_few_rows<T, 1, 2, 4>(p, waves, stream) : launch_few_rows<T, 2, 2, 3>(p, waves, stream);
-        return launch_few_rows<T, 1, 4, 3>(p, waves, stream);
+        if (p.N <= 8) return narrow ? launch_patch<T, 1, 1, 4>(p, waves, stream) : launch_patch<T, 2, 1, 3>(p, waves, stream);
+        return narrow ? launch_patch<T, 1, 2, 4>(p, waves, stream) : launch_patch<T, 2, 2, 3>(p, waves, stream);
     }
     const FormPrice& f = kFormPrices[form];
     if (((int64_t)p.N + f.rows - 1) / f.rows * ((p.F + f.columns - 1) / f.columns) >= (INT64_C(1) << 22)) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
@@ -750,6 +754,10 @@ static int32_t linear_launch(const LinearParams& p, hipStream_t stream) {
         case kTwoPerCu: return launch_ring<T, 4, 4, 2, 1>(p, stream);
         case kBlock: return launch_block<T, 2, 2, 4>(p, stream);
         case kTallBlock: return launch_block<T, 2, 3, 4>(p, stream);
+        case kPatch16: return launch_patch<T, 1, 2, 4>(p, 8, stream);
+        case kPatch16x32: return launch_patch<T, 1, 4, 3>(p, 8, stream);
+        case kPatch32: return launch_patch<T, 2, 4, 3>(p, 4, stream);
+        case kPatch64x32: return launch_patch<T, 4, 4, 3>(p, 4, stream);
         default: return p.D % 64 ? launch_wide<T, true>(p, stream) : launch_wide<T, false>(p, stream);
     }
 }

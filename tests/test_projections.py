@@ -84,7 +84,8 @@ def _check_linear(cm, N, D, F, dtype, act, bias=True, residual=True, seed=0, spr
 SIZES = [(1, 8, 8), (1, 264, 72), (2, 256, 5120), (3, 4096, 1000), (5, 72, 16), (15, 1032, 520), (16, 640, 136), (17, 2056, 264), (31, 512, 2048),
          (33, 4104, 88), (64, 1024, 1024), (65, 64, 64), (100, 5120, 24), (127, 576, 392), (200, 8, 640), (255, 1536, 768), (256, 256, 256),
          (257, 320, 2056), (500, 3000, 1288), (1000, 128, 5000), (2049, 1000, 2000), (4608, 640, 1920)]
-MORE_SIZES = [(100, 1040, 13392), (380, 392, 10880), (900, 4360, 2544), (450, 200, 10880), (2100, 968, 8200), (1500, 1016, 3000), (513, 72, 12296), (33, 8200, 264)]
+MORE_SIZES = [(100, 1040, 13392), (380, 392, 10880), (900, 4360, 2544), (450, 200, 10880), (2100, 968, 8200), (1500, 1016, 3000), (513, 72, 12296), (33, 8200, 264),
+              (130, 5056, 640), (77, 1544, 1000), (300, 2056, 1000), (45, 640, 3496), (601, 1096, 520), (289, 4104, 1000), (33, 72, 24)]
 
 
 @gpu
@@ -180,8 +181,8 @@ def test_linear_beyond_32_bits(cm):
 def test_every_form_of_tiles_is_reached(cm):
     """From one row to thousands; the sizes of test_linear take each form."""
     form = cm.load().chipmunk_internal_linear_form
-    assert form(1, 4096, 4096) == form(16, 64, 30720) == form(32, 4096, 4096) == 7 and form(17, 4096, 30720) < 7
-    assert {form(N, D, F) for N, D, F in SIZES + MORE_SIZES} == set(range(8))
+    assert form(1, 4096, 4096) == form(16, 64, 30720) == 11 and form(400, 4096, 4096) < 7 <= form(17, 4096, 1024) < 11
+    assert {form(N, D, F) for N, D, F in SIZES + MORE_SIZES} == set(range(12))
 
 
 def test_no_accumulator_is_touched_before_its_product_has_landed(tmp_path):
