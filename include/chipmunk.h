@@ -273,7 +273,8 @@ int32_t chipmunk_mlp_dense(const uint16_t* x, const uint16_t* w1, const uint16_t
 
 /* ---- The attention half of a block around the kernels above, and a text encoder's: projections, rotary positions, and
  * attention over packed sequences.  Elements are bf16 or fp16 (dtype), raw 16-bit values as above; strides are in elements,
- * multiples of 8, of rows that do not overlap (a stride along a size of one does not count); positions and lengths are on the device, and no call reads them on the host. ---- */
+ * multiples of 8, of rows that do not overlap (a stride along a size of one does not count); positions and lengths are on the
+ * device, and no call reads them on the host. ---- */
 
 #define CHIPMUNK_DTYPE_BF16  0
 #define CHIPMUNK_DTYPE_FP16  1
@@ -288,7 +289,8 @@ int32_t chipmunk_mlp_dense(const uint16_t* x, const uint16_t* w1, const uint16_t
  * row stride ldr, or NULL; out: [N,F], row stride ldo.  out may be residual
  * (same pointer and stride) and overlaps nothing else.  The values between a
  * row's end and the next row are neither read nor written.  D and F multiples
- * of 8, D < 2^20, row strides < 2^22.  silu(y) = y / (1 + exp(-y)). */
+ * of 8, D < 2^20, row strides < 2^22, out fewer than 2^22 tiles of 256 x 256.
+ * silu(y) = y / (1 + exp(-y)). */
 int32_t chipmunk_linear(const uint16_t* x, int64_t ldx, const uint16_t* w, const uint16_t* bias,
                         const uint16_t* residual, int64_t ldr, uint16_t* out, int64_t ldo,
                         int N, int D, int F, int act, int dtype, void* stream);
@@ -313,10 +315,10 @@ int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_head_
  *   out[i,h] = softmax_j(softmax_scale * <q[i,h], k[j]>) v[j]     over the keys that are seen; none: zero.
  * Scores, softmax and sums are fp32; a probability is rounded to the element type where it meets v, and so in its sum.  Keys that
  * a query does not see have no influence on it, whatever k and v hold there.
- * q, k, v, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E.  Tq, Tk: rows of q (and out) and of k and v.  Rows of out that belong to no sequence are
- * left as they were.  max_q, max_k: no sequence has more queries, keys; sequences that do are cut there, which gives wrong
- * results.  cu_q, cu_k: [S+1] int32 ascending; with k_len, cu_k[S] is not read.  Entries are clamped so that bad ones give wrong
- * results, not accesses outside the tensors.
+ * q, k, v, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E.  Tq, Tk:
+ * rows of q (and out) and of k and v.  Rows of out that belong to no sequence are left as they were.  max_q, max_k: no sequence
+ * has more queries, keys; sequences that do are cut there, which gives wrong results.  cu_q, cu_k: [S+1] int32 ascending; with
+ * k_len, cu_k[S] is not read.  Entries are clamped so that bad ones give wrong results, not accesses outside the tensors.
  * E in {64,128}; token strides < 2^24.  ws: chipmunk_attn_packed_workspace_bytes() (0: ws may be NULL; also 0 on bad
  * arguments), contents undefined afterwards, not to be shared by calls that may overlap. */
 size_t chipmunk_attn_packed_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k);

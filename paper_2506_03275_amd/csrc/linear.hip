@@ -6,6 +6,7 @@
 #include "element.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace chipmunk {
@@ -23,7 +24,21 @@ struct LinearParams {
 
 template <int ACT>
 __device__ __forceinline__ float activation(float y) {
-    if constexpr (ACT == CHIPMUNK_ACT_GELU_ERF) return 0.5f * y * (1.f + erff(y * 0.70710678118654752f));
+    // x (1 + erf(x / sqrt 2)) / 2 = max(x, 0) - |x| h(|x|), h(z) = erfc(z / sqrt 2) / 2 = exp(-z^2 / 2) t P(t) with t = 1 / (1 + 0.362 z).
+    // P was fitted here to the least relative error, 7.6e-7 over all z; with the rounding of 32 bits the result is off by 2.4e-7 at
+    // most.  With erff, two branches that a wave mostly takes both, the results cost more than the product: 2148 rows, 256 -> 8192,
+    // 53.6 us, now 31.7 (no activation: 22.8).  The bound on |x| keeps an infinite one from 0 times infinity.
+    if constexpr (ACT == CHIPMUNK_ACT_GELU_ERF) {
+        const float z = fminf(fabsf(y), 30.f), t = __builtin_amdgcn_rcpf(__builtin_fmaf(z, 0.362f, 1.f));
+        float h = 0.047938276f;
+        h = __builtin_fmaf(h, t, -0.18000965f);
+        h = __builtin_fmaf(h, t, 0.17661723f);
+        h = __builtin_fmaf(h, t, 0.0288315f);
+        h = __builtin_fmaf(h, t, 0.13942969f);
+        h = __builtin_fmaf(h, t, 0.14268932f);
+        h = __builtin_fmaf(h, t, 0.1445039f) * t * __builtin_amdgcn_exp2f(y * y * -0.72134752f);
+        return __builtin_fmaf(-z, h, fmaxf(y, 0.f));
+    }
     // x (1 + tanh(u)) / 2 = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3);  -2 u log2(e) = x (A + B x^2).  The reciprocal
     // and the exponential are an ulp of 32 bits off, and the result has 8 or 11 bits.
     if constexpr (ACT == CHIPMUNK_ACT_GELU_TANH)
@@ -716,17 +731,19 @@ static const FormPrice kFormPrices[kForms] = {{64, 64, 512, 1, 1.5f, 0.24f, 0.20
                                               {128, 128, 512, 1, 3.0f, 0.56f, 0.45f}, {128, 128, 256, 1, 2.8f, 0.36f, 0.20f}, {128, 192, 256, 1, 3.4f, 0.48f, 0.29f},
                                               {256, 256, 256, 1, 6.0f, 1.00f, 0.45f}, {16, 16, 256, 8, 2.05f, 0.37f, 0.0f},   {16, 32, 256, 8, 2.18f, 0.47f, 0.05f},
                                               {32, 32, 256, 4, 2.55f, 0.32f, 0.09f},  {64, 32, 256, 4, 3.05f, 0.50f, 0.18f}};
+constexpr int64_t kMostTiles = 1 << 22;                   // a launch has fewer than 2^32 threads
 static double price_of(Form form, int64_t N, int64_t D, int64_t F) {
     const FormPrice& f = kFormPrices[form];
     const int64_t tiles = (N + f.rows - 1) / f.rows * ((F + f.columns - 1) / f.columns), steps = ((D + 63) / 64 + f.parts - 1) / f.parts;
     const int64_t whole = tiles / f.per_round, rest = tiles % f.per_round;
+    if (tiles >= kMostTiles) return HUGE_VAL;
     return whole * (f.round + steps * (double)(f.step + f.beside)) + (rest ? f.round + steps * (f.step + f.beside * (double)rest / f.per_round) : 0.0);
 }
 
 // Up to 16 rows there is nothing to choose: a patch of all rows reads the weights once, at the memory's rate (4096 x 4096, one row:
 // 7.4 us, tiles 13.5).
 static Form linear_form(int N, int D, int F) {
-    if (N <= 16) return kFewRows;
+    if (N <= 16 && F / 16 < kMostTiles) return kFewRows;
     Form best = kSmall;
     for (int f = 1; f < kForms; f++)
         if (price_of((Form)f, N, D, F) < price_of(best, N, D, F)) best = (Form)f;
@@ -745,8 +762,7 @@ static int32_t linear_launch(const LinearParams& p, hipStream_t stream) {
         if (p.N <= 8) return narrow ? launch_patch<T, 1, 1, 4>(p, waves, stream) : launch_patch<T, 2, 1, 3>(p, waves, stream);
         return narrow ? launch_patch<T, 1, 2, 4>(p, waves, stream) : launch_patch<T, 2, 2, 3>(p, waves, stream);
     }
-    const FormPrice& f = kFormPrices[form];
-    if (((int64_t)p.N + f.rows - 1) / f.rows * ((p.F + f.columns - 1) / f.columns) >= (INT64_C(1) << 22)) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
+    if (price_of(form, p.N, p.D, p.F) == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;
     switch (form) {
         case kSmall: return launch_ring<T, 2, 2, 4, 1>(p, stream);
         case kSmallTeams: return launch_ring<T, 2, 2, 4, 2>(p, stream);

@@ -183,6 +183,11 @@ def test_every_form_of_tiles_is_reached(cm):
     form = cm.load().chipmunk_internal_linear_form
     assert form(1, 4096, 4096) == form(16, 64, 30720) == 11 and form(400, 4096, 4096) < 7 <= form(17, 4096, 1024) < 11
     assert {form(N, D, F) for N, D, F in SIZES + MORE_SIZES} == set(range(12))
+    # a result so long that one launch does not cover it with small tiles has larger ones
+    sizes = [(64, 64), (64, 64), (64, 128), (128, 128), (128, 128), (128, 192), (256, 256), (16, 16), (16, 32), (32, 32), (64, 32)]
+    for N, F in ((2 ** 29, 8), (2 ** 30 - 256, 8), (8, 2 ** 29), (16, 2 ** 30 - 256)):
+        columns, rows = sizes[form(N, 8, F)]
+        assert -(-N // rows) * -(-F // columns) < 2 ** 22
 
 
 def test_no_accumulator_is_touched_before_its_product_has_landed(tmp_path):
