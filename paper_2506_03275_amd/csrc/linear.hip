@@ -718,8 +718,8 @@ static int32_t launch_patch(LinearParams p, int waves, hipStream_t stream) {
 
 // The forms of tiles.  A launch is priced in us as rounds of as many tiles as the CUs hold: each round has its start and end, and
 // for every contraction step what it takes alone and what the tiles beside it add; the last, partly filled round counts by its
-// share.  Measured per form on launches of 1 to 18 000 rows and contractions of 256 to 8192; on 1982 random ones of 17 to 1500 rows
-// and 256 to 20 000 columns the form taken is 1.014 times the quickest's time in the mean, 1.28 at most.  The small forms whose
+// share.  Fitted to 5901 random sizes, 17 to 30 000 rows, contractions of 256 to 8192, 256 to 30 720 columns: the form taken is 1.005
+// times the quickest's time in the mean, 1.25 at most; of 1019 others 1.004 and 1.18.  The small forms whose
 // waves divide the contraction are for few tiles: 190 rows, 4992 -> 520: 8.3 us by 16 x 32, 16.2 by the quickest other; 4032 -> 464
 // with 21 rows 4.7 and 12.9; 236 rows, 5440 -> 3480 29.4 and 20.4.
 enum Form { kSmall, kSmallTeams, kMiddleTeams, kTwoPerCu, kBlock, kTallBlock, kWide, kPatch16, kPatch16x32, kPatch32, kPatch64x32, kForms, kFewRows = kForms };
@@ -727,10 +727,10 @@ struct FormPrice {
     int columns, rows, per_round, parts;                  // parts: of the contraction, a wave's each
     float round, step, beside;
 };
-static const FormPrice kFormPrices[kForms] = {{64, 64, 512, 1, 1.5f, 0.24f, 0.20f},   {64, 64, 256, 1, 2.3f, 0.165f, 0.06f}, {64, 128, 256, 1, 2.4f, 0.25f, 0.07f},
-                                              {128, 128, 512, 1, 3.0f, 0.56f, 0.45f}, {128, 128, 256, 1, 2.8f, 0.36f, 0.20f}, {128, 192, 256, 1, 3.4f, 0.48f, 0.29f},
-                                              {256, 256, 256, 1, 6.0f, 1.00f, 0.45f}, {16, 16, 256, 8, 2.05f, 0.37f, 0.0f},   {16, 32, 256, 8, 2.18f, 0.47f, 0.05f},
-                                              {32, 32, 256, 4, 2.55f, 0.32f, 0.09f},  {64, 32, 256, 4, 3.05f, 0.50f, 0.18f}};
+static const FormPrice kFormPrices[kForms] = {{64, 64, 512, 1, 1.65f, 0.24f, 0.20f},  {64, 64, 256, 1, 2.78f, 0.18f, 0.09f},  {64, 128, 256, 1, 2.4f, 0.26f, 0.075f},
+                                              {128, 128, 512, 1, 2.47f, 0.56f, 0.44f}, {128, 128, 256, 1, 2.62f, 0.36f, 0.20f}, {128, 192, 256, 1, 3.6f, 0.51f, 0.31f},
+                                              {256, 256, 256, 1, 7.15f, 1.02f, 0.42f}, {16, 16, 256, 8, 2.05f, 0.385f, 0.0f},  {16, 32, 256, 8, 1.98f, 0.50f, 0.057f},
+                                              {32, 32, 256, 4, 2.3f, 0.246f, 0.07f},   {64, 32, 256, 4, 3.44f, 0.364f, 0.20f}};
 constexpr int64_t kMostTiles = 1 << 22;                   // a launch has fewer than 2^32 threads
 static double price_of(Form form, int64_t N, int64_t D, int64_t F) {
     const FormPrice& f = kFormPrices[form];
