@@ -114,6 +114,37 @@ def test_heads(cm, Hq, Hk, causal):
     _check(cm, [1, 1, 2], [260, 7, 130], Hq, Hk, 128, torch.float16, causal)
 
 
+# one batch for each form that takes whole tiles of queries: rows of a tile / 64 + 1
+FORMS = [(64, False, 3, 40, 40, [701, 0, 700, 129, 301, 1, 64, 700]), (64, False, 4, 32, 8, [4003, 1, 0, 70]), (64, True, 2, 40, 40, [130, 60, 0, 1]),
+         (64, True, 3, 40, 40, [1201, 701, 1, 1201, 33, 701, 0, 701, 701]), (64, True, 4, 64, 8, [8003, 1, 0, 70]), (128, False, 2, 40, 40, [130, 60, 0, 1]),
+         (128, False, 3, 32, 8, [301, 301, 0, 301, 301, 1]), (128, False, 4, 64, 8, [1503, 1, 64, 0]), (128, True, 3, 40, 40, [301, 1, 301, 301, 301, 0]),
+         (128, True, 4, 32, 8, [4003, 0, 1, 31])]
+
+
+def test_the_forms_are_what_the_batches_take(cm):
+    form = cm.load().chipmunk_internal_attn_packed_form
+    for E, causal, want, Hq, Hk, lengths in FORMS:
+        assert form(len(lengths), sum(lengths), Hq, Hk, E, max(lengths), max(lengths), causal) == want
+
+
+@gpu
+@pytest.mark.parametrize("E,causal,form,Hq,Hk,lengths", FORMS)
+def test_large_batches(cm, E, causal, form, Hq, Hk, lengths):
+    for dtype in TYPES:
+        q, k, v, cu_q, cu_k, _ = _inputs(lengths, lengths, Hq, Hk, E, dtype, form, packed=True)
+        out = _run(cm, q, k, v, cu_q, cu_k, None, lengths, lengths, causal, E ** -0.5)
+        assert not bool(out.isnan().any())
+        for s, n in enumerate(lengths):
+            rows = slice(int(cu_q[s]), int(cu_q[s]) + n)
+            for h in (0, Hq // 2 + 1, Hq - 1):
+                g = h // (Hq // Hk)
+                want, off = reference(q[rows, h:h + 1], k[rows, g:g + 1], v[rows, g:g + 1], causal, E ** -0.5)
+                got = out[rows, h:h + 1].double()
+                assert bool(((got - want).abs() <= off).all()), (s, n, h)
+        again = _run(cm, q, k, v, cu_q, cu_k, None, lengths, lengths, causal, E ** -0.5)
+        assert torch.equal(again, out)
+
+
 CONTINUED = [([5], [70]), ([1], [1]), ([1], [64]), ([1], [65]), ([1, 1, 1], [1, 4000, 129]), ([17, 3], [200, 3]), ([150], [1000]), ([64, 0, 9], [64, 30, 0]),
              ([300, 2], [100, 1]), ([200], [1]), ([4, 4, 4, 4], [4, 5, 600, 0]), ([1] * 40, list(range(0, 2000, 50))), ([130, 1, 33], [129, 900, 31]), ([8], [5000]), ([1], [9001])]
 
