@@ -57,5 +57,24 @@ __device__ __forceinline__ void from_columns_32(u32x4 columns, u32x2 (&run)[2]) 
     run[0] = u32x2{lo[0], hi[0]};
     run[1] = u32x2{lo[1], hi[1]};
 }
+// Lanes 8 apart in a row of 16 exchange: `first` then holds both of the lower lane, side by side, `second` both of the upper one.
+// (row_ror:8; the banks of four lanes that are written are 2 and 3, then 0 and 1.)
+__device__ __forceinline__ void exchange_8_apart(u32x4& first, u32x4& second) {
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const uint32_t a = first[w], b = second[w];
+        first[w] = (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x128, 0xf, 0xc, false);
+        second[w] = (uint32_t)__builtin_amdgcn_update_dpp((int)b, (int)a, 0x128, 0xf, 0x3, false);
+    }
+}
+// The same of lanes 16 apart in a half of 32.
+__device__ __forceinline__ void exchange_16_apart(u32x4& first, u32x4& second) {
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const auto both = __builtin_amdgcn_permlane16_swap(first[w], second[w], false, false);
+        first[w] = both[0];
+        second[w] = both[1];
+    }
+}
 
 }  // namespace chipmunk

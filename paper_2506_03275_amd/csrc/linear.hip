@@ -19,6 +19,7 @@ struct LinearParams {
     uint16_t* out;
     int64_t ldx, ldr, ldo;
     int N, D, F, act;
+    int past;                // LinearPast
     int tiles_p, tiles_q;
 };
 
@@ -85,6 +86,28 @@ __device__ __forceinline__ bool linear_tile(int tiles_p, int tiles_q, int* tp, i
     return true;
 }
 
+// The result from (row0, col0) on, for 16-byte stores of `rows` rows at most; what lies at kNowhere is not stored.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t result_rows(const LinearParams& p, int row0, int col0, int rows) {
+    const int there = col0 < p.F ? max(min(rows, p.N - row0), 0) : 0;
+    return raw_buffer(p.out + (int64_t)row0 * p.ldo + col0, there > 0 ? (uint32_t)((there - 1) * p.ldo + p.F - col0) * 2u : 0u);
+}
+// A result whose rows are whole lines of 128 bytes is written through the L2s as it comes, and past the last-level cache where it is larger
+// than that; other lines come in parts, which meet in an L2 (64 columns of a row at a time; us with a kernel that reads the result,
+// kept in the L2s / written through / past the last-level cache: 8000 x 4096 60.3, 56.2, 64.2; 32 768 x 2048 105, 99, 103; 75 600 x 5120
+// 696, 673, 633; 16 000 x 3000 78, 98, 86).
+enum LinearPast { kKept, kThrough, kPastLastLevel };
+constexpr int64_t kLinearLastLevel = 256 << 20;
+template <int N>
+__device__ __forceinline__ void store_16B(const u32x4 (&values)[N], __amdgpu_buffer_rsrc_t to, const uint32_t (&offsets)[N], int past) {
+    auto store = [&](auto bits) {
+#pragma unroll
+        for (int n = 0; n < N; n++) __builtin_amdgcn_raw_buffer_store_b128(values[n], to, (int)offsets[n], 0, decltype(bits)::value);
+    };
+    if (past == kKept) store(std::integral_constant<int, 0>{});
+    else if (past == kThrough) store(std::integral_constant<int, 16>{});   // sc1
+    else store(std::integral_constant<int, 2>{});                          // nt
+}
+
 // Results of a wave: PB x QB blocks of 16 columns x 16 rows from (col0, row0) on.
 template <class T, int ACT, int PB, int QB>
 __device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 (&acc)[PB][QB], int col0, int row0, int g, int l16) {
@@ -104,34 +127,51 @@ __device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 
         }
         return;
     }
-#pragma unroll
-    for (int pair = 0; pair < PB / 2; pair++) {
-        const int col = col0 + pair * 32;
-        u32x2 bias[2] = {u32x2{0, 0}, u32x2{0, 0}};
-        if (p.bias) {
-#pragma unroll
-            for (int i = 0; i < 2; i++) bias[i] = *reinterpret_cast<const u32x2*>(p.bias + min(col + i * 16 + 4 * g, p.F - 4));
+    // the lane's eight columns, from `at` on, of block c of rows and of one pair of blocks of columns
+    auto eight_columns = [&](int pair, int c, const u32x2 (&bias)[2], int at, int row, bool there) {
+        u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
+        if (p.residual) {
+            u32x4 r = {0, 0, 0, 0};
+            if (there) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
+            from_columns(r, old);
         }
-        const int at = col + columns_of_lane(g);
+        u32x2 result[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            f32x4 v = acc[2 * pair + i][c];
+            // (the widest tiles' sums stay in their accumulation registers up to here: copied ahead of the activations' branches they would spill)
+            if (PB * QB == 8) asm volatile("" : "+a"(v));
+            result[i] = u32x2{T::pack(activation<ACT>(v[0] + T::low(bias[i][0])) + T::low(old[i][0]), activation<ACT>(v[1] + T::high(bias[i][0])) + T::high(old[i][0])),
+                              T::pack(activation<ACT>(v[2] + T::low(bias[i][1])) + T::low(old[i][1]), activation<ACT>(v[3] + T::high(bias[i][1])) + T::high(old[i][1]))};
+        }
+        return to_columns(result[0], result[1]);
+    };
+    const __amdgpu_buffer_rsrc_t to = result_rows(p, row0, col0, QB * 16);
+    constexpr int PAIRS = PB % 4 == 0 ? 2 : 1;            // at a time: 64 columns are 128 bytes, and rows of whole lines are stored
+#pragma unroll
+    for (int pair = 0; pair < PB / 2; pair += PAIRS) {
+        const int col = col0 + pair * 32;
+        u32x2 bias[PAIRS][2];
+#pragma unroll
+        for (int n = 0; n < PAIRS; n++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) bias[n][i] = p.bias ? *reinterpret_cast<const u32x2*>(p.bias + min(col + n * 32 + i * 16 + 4 * g, p.F - 4)) : u32x2{0, 0};
 #pragma unroll
         for (int c = 0; c < QB; c++) {
-            const int row = row0 + c * 16 + l16;
-            const bool there = row < p.N && at < p.F;
-            u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
-            if (p.residual) {
-                u32x4 r = {0, 0, 0, 0};
-                if (there) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
-                from_columns(r, old);
-            }
-            u32x2 result[2];
+            u32x4 columns[PAIRS];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const f32x4 v = acc[2 * pair + i][c];
-                result[i] = u32x2{T::pack(activation<ACT>(v[0] + T::low(bias[i][0])) + T::low(old[i][0]), activation<ACT>(v[1] + T::high(bias[i][0])) + T::high(old[i][0])),
-                                  T::pack(activation<ACT>(v[2] + T::low(bias[i][1])) + T::low(old[i][1]), activation<ACT>(v[3] + T::high(bias[i][1])) + T::high(old[i][1]))};
+            for (int n = 0; n < PAIRS; n++) {
+                const int at = col + n * 32 + columns_of_lane(g), row = row0 + c * 16 + l16;
+                columns[n] = eight_columns(pair + n, c, bias[n], at, row, row < p.N && at < p.F);
             }
-            const u32x4 columns = to_columns(result[0], result[1]);
-            if (there) *reinterpret_cast<u32x4*>(p.out + (int64_t)row * p.ldo + at) = columns;
+            if constexpr (PAIRS == 2) exchange_8_apart(columns[0], columns[1]);
+            uint32_t offset[PAIRS];
+#pragma unroll
+            for (int n = 0; n < PAIRS; n++) {
+                const int at = pair * 32 + columns_of_lane(g) + (PAIRS == 2 ? (l16 >> 3) * 32 : 0), row = c * 16 + (PAIRS == 2 ? n * 8 + (l16 & 7) : l16);
+                offset[n] = row0 + row < p.N && col0 + at < p.F ? (uint32_t)(row * (uint32_t)p.ldo + at) * 2u : kNowhere;
+            }
+            store_16B(columns, to, offset, PAIRS == 2 ? p.past : kKept);
             if (PB * QB == 8) __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -147,37 +187,49 @@ __device__ __forceinline__ void linear_store_32(const LinearParams& p, const f32
     const int high = lane >> 5;
     with_activation(p.act, [&](auto form) {
         constexpr int ACT = decltype(form)::value;
+        static_assert(PN == 2, "64 columns: rows of whole lines of 128 bytes are stored");
+        const __amdgpu_buffer_rsrc_t to = result_rows(p, row0, col0, QN * 32);
+        u32x2 bias[4][2];                                // of the lane's first run and its second of each 16 columns
 #pragma unroll
-        for (int a = 0; a < PN; a++)
+        for (int m = 0; m < 4; m++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const int col = col0 + a * 32 + j * 16, at = col + 8 * high;   // of the lane's first run; of its eight columns
-                u32x2 bias[2] = {u32x2{0, 0}, u32x2{0, 0}};
-                if (p.bias) {
+            for (int i = 0; i < 2; i++) bias[m][i] = p.bias ? *reinterpret_cast<const u32x2*>(p.bias + min(col0 + m * 16 + i * 8 + 4 * high, p.F - 4)) : u32x2{0, 0};
 #pragma unroll
-                    for (int i = 0; i < 2; i++) bias[i] = *reinterpret_cast<const u32x2*>(p.bias + min(col + i * 8 + 4 * high, p.F - 4));
+        for (int c = 0; c < QN; c++) {
+            u32x4 columns[4];
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                const int row = row0 + c * 32 + (lane & 31), at = col0 + m * 16 + 8 * high;
+                u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
+                if (p.residual) {
+                    u32x4 r = {0, 0, 0, 0};
+                    if (row < p.N && at < p.F) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
+                    from_columns_32(r, old);
                 }
+                u32x2 result[2];
 #pragma unroll
-                for (int c = 0; c < QN; c++) {
-                    const int row = row0 + c * 32 + (lane & 31);
-                    const bool there = row < p.N && at < p.F;
-                    u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
-                    if (p.residual) {
-                        u32x4 r = {0, 0, 0, 0};
-                        if (there) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
-                        from_columns_32(r, old);
+                for (int i = 0; i < 2; i++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const int e = 8 * (m & 1) + 4 * i + 2 * h;
+                        result[i][h] = T::pack(activation<ACT>(acc[m >> 1][c][e] + T::low(bias[m][i][h])) + T::low(old[i][h]),
+                                               activation<ACT>(acc[m >> 1][c][e + 1] + T::high(bias[m][i][h])) + T::high(old[i][h]));
                     }
-                    u32x2 result[2];
-#pragma unroll
-                    for (int i = 0; i < 2; i++)
-#pragma unroll
-                        for (int h = 0; h < 2; h++)
-                            result[i][h] = T::pack(activation<ACT>(acc[a][c][8 * j + 4 * i + 2 * h] + T::low(bias[i][h])) + T::low(old[i][h]),
-                                                   activation<ACT>(acc[a][c][8 * j + 4 * i + 2 * h + 1] + T::high(bias[i][h])) + T::high(old[i][h]));
-                    const u32x4 columns = to_columns_32(result[0], result[1]);
-                    if (there) *reinterpret_cast<u32x4*>(p.out + (int64_t)row * p.ldo + at) = columns;
-                }
+                columns[m] = to_columns_32(result[0], result[1]);
             }
+            // rows of the 32 by their bits 4 and 3: columns[2 * bit 4 + bit 3] afterwards, the 16 columns by the lane's
+            exchange_8_apart(columns[0], columns[1]);
+            exchange_8_apart(columns[2], columns[3]);
+            exchange_16_apart(columns[0], columns[2]);
+            exchange_16_apart(columns[1], columns[3]);
+            uint32_t offset[4];
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                const int row = c * 32 + m * 8 + (lane & 7), at = (lane >> 3 & 3) * 16 + 8 * high;
+                offset[m] = row0 + row < p.N && col0 + at < p.F ? (uint32_t)(row * (uint32_t)p.ldo + at) * 2u : kNowhere;
+            }
+            store_16B(columns, to, offset, p.past);
+        }
     });
 }
 
@@ -311,17 +363,6 @@ __global__ __launch_bounds__(256 * TEAMS, 2) void linear_ring_kernel(LinearParam
                 for (int a = 0; a < PB; a++) total[a][0] += sums[(((v * 4 + w) * PB + a) * QB + c) * 64 + lane];
             linear_store<T, PB, 1>(p, total, col0, row0 + c * 16, g, l16);
         }
-    }
-}
-
-// Waits until at most `left` steps of N transfers each are outstanding; there are MOST of them at most.
-template <int N, int MOST>
-__device__ __forceinline__ void wait_steps_of(int left) {
-    if constexpr (MOST == 0) {
-        wait_vmem_at_most<0>();
-    } else {
-        if (left >= MOST) wait_vmem_at_most<N * MOST>();
-        else wait_steps_of<N, MOST - 1>(left);
     }
 }
 
@@ -799,6 +840,8 @@ extern "C" int32_t chipmunk_linear(const uint16_t* x, int64_t ldx, const uint16_
         return CHIPMUNK_ERR_UNSUPPORTED;
     if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(residual) || !aligned16(out) || (ldx | ldo | (residual ? ldr : 0)) % 8 != 0)
         return CHIPMUNK_ERR_ALIGN;
-    const LinearParams p{x, w, bias, residual, out, ldx, ldr, ldo, N, D, F, act, 0, 0};
+    const bool whole_lines = ldo % 64 == 0 && (reinterpret_cast<uintptr_t>(out) & 127) == 0;
+    const int past = !whole_lines ? kKept : (int64_t)N * F * 2 > kLinearLastLevel ? kPastLastLevel : kThrough;
+    const LinearParams p{x, w, bias, residual, out, ldx, ldr, ldo, N, D, F, act, past, 0, 0};
     return dtype == CHIPMUNK_DTYPE_BF16 ? linear_launch<Bf16>(p, static_cast<hipStream_t>(stream)) : linear_launch<Fp16>(p, static_cast<hipStream_t>(stream));
 }
