@@ -86,11 +86,12 @@ __device__ __forceinline__ bool linear_tile(int tiles_p, int tiles_q, int* tp, i
     return true;
 }
 
-// The result from (row0, col0) on, for 16-byte stores of `rows` rows at most; what lies at kNowhere is not stored.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t result_rows(const LinearParams& p, int row0, int col0, int rows) {
+// The result or the residual from (row0, col0) on, for 16-byte accesses to `rows` rows at most; nothing is read or stored at kNowhere.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const LinearParams& p, const uint16_t* base, int64_t ld, int row0, int col0, int rows) {
     const int there = col0 < p.F ? max(min(rows, p.N - row0), 0) : 0;
-    return raw_buffer(p.out + (int64_t)row0 * p.ldo + col0, there > 0 ? (uint32_t)((there - 1) * p.ldo + p.F - col0) * 2u : 0u);
+    return raw_buffer(base + (int64_t)row0 * ld + col0, there > 0 ? (uint32_t)((there - 1) * ld + p.F - col0) * 2u : 0u);
 }
+__device__ __forceinline__ u32x4 load_16B(__amdgpu_buffer_rsrc_t from, uint32_t offset) { return __builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0); }
 // A result whose rows are whole lines of 128 bytes is written through the L2s as it comes, and past the last-level cache where it is larger
 // than that; other lines come in parts, which meet in an L2 (64 columns of a row at a time; us with a kernel that reads the result,
 // kept in the L2s / written through / past the last-level cache: 8000 x 4096 60.3, 56.2, 64.2; 32 768 x 2048 105, 99, 103; 75 600 x 5120
@@ -108,33 +109,35 @@ __device__ __forceinline__ void store_16B(const u32x4 (&values)[N], __amdgpu_buf
     else store(std::integral_constant<int, 2>{});                          // nt
 }
 
-// Results of a wave: PB x QB blocks of 16 columns x 16 rows from (col0, row0) on.
-template <class T, int ACT, int PB, int QB>
-__device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 (&acc)[PB][QB], int col0, int row0, int g, int l16) {
-    static_assert(PB % 2 == 0 || PB == 1, "blocks of columns go in pairs");
-    if constexpr (PB == 1) {                              // four columns of a lane at a time
-        const int at = col0 + 4 * g;
-        const u32x2 bias = p.bias ? *reinterpret_cast<const u32x2*>(p.bias + min(at, p.F - 4)) : u32x2{0, 0};
+// Results of a wave: PB x QB blocks of 16 columns x 16 rows from (col0, row0) on.  The residual's values there come ahead of them: loaded
+// block by block, one latency behind the other, they took 60 us of 18 000 rows, 5120 -> 5120 (732 us, now NOW).
+template <int PB, int QB>
+struct Residual {
+    u32x4 of[PB / 2][QB];                                 // a lane's eight columns of each pair of blocks
+};
+template <int PB, int QB>
+__device__ __forceinline__ void load_residual(Residual<PB, QB>& old, const LinearParams& p, int col0, int row0, int g, int l16) {
+#pragma unroll
+    for (int pair = 0; pair < PB / 2; pair++)
+#pragma unroll
+        for (int c = 0; c < QB; c++) old.of[pair][c] = u32x4{0, 0, 0, 0};
+    if (!p.residual) return;
+    const __amdgpu_buffer_rsrc_t from = rows_from(p, p.residual, p.ldr, row0, col0, QB * 16);
+#pragma unroll
+    for (int pair = 0; pair < PB / 2; pair++)
 #pragma unroll
         for (int c = 0; c < QB; c++) {
-            const int row = row0 + c * 16 + l16;
-            if (row >= p.N || at >= p.F) continue;
-            const u32x2 old = p.residual ? *reinterpret_cast<const u32x2*>(p.residual + (int64_t)row * p.ldr + at) : u32x2{0, 0};
-            const f32x4 v = acc[0][c];
-            *reinterpret_cast<u32x2*>(p.out + (int64_t)row * p.ldo + at) =
-                u32x2{T::pack(activation<ACT>(v[0] + T::low(bias[0])) + T::low(old[0]), activation<ACT>(v[1] + T::high(bias[0])) + T::high(old[0])),
-                      T::pack(activation<ACT>(v[2] + T::low(bias[1])) + T::low(old[1]), activation<ACT>(v[3] + T::high(bias[1])) + T::high(old[1]))};
+            const int row = c * 16 + l16, at = pair * 32 + columns_of_lane(g);
+            old.of[pair][c] = load_16B(from, row0 + row < p.N && col0 + at < p.F ? (uint32_t)(row * (uint32_t)p.ldr + at) * 2u : kNowhere);
         }
-        return;
-    }
-    // the lane's eight columns, from `at` on, of block c of rows and of one pair of blocks of columns
-    auto eight_columns = [&](int pair, int c, const u32x2 (&bias)[2], int at, int row, bool there) {
-        u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
-        if (p.residual) {
-            u32x4 r = {0, 0, 0, 0};
-            if (there) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
-            from_columns(r, old);
-        }
+}
+template <class T, int ACT, int PB, int QB>
+__device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 (&acc)[PB][QB], const Residual<PB, QB>& residual, int col0, int row0, int g, int l16) {
+    static_assert(PB % 2 == 0, "blocks of columns go in pairs");
+    // the lane's eight columns of block c of rows and of one pair of blocks of columns
+    auto eight_columns = [&](int pair, int c, const u32x2 (&bias)[2]) {
+        u32x2 old[2];
+        from_columns(residual.of[pair][c], old);
         u32x2 result[2];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
@@ -146,7 +149,7 @@ __device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 
         }
         return to_columns(result[0], result[1]);
     };
-    const __amdgpu_buffer_rsrc_t to = result_rows(p, row0, col0, QB * 16);
+    const __amdgpu_buffer_rsrc_t to = rows_from(p, p.out, p.ldo, row0, col0, QB * 16);
     constexpr int PAIRS = PB % 4 == 0 ? 2 : 1;            // at a time: 64 columns are 128 bytes, and rows of whole lines are stored
 #pragma unroll
     for (int pair = 0; pair < PB / 2; pair += PAIRS) {
@@ -160,10 +163,7 @@ __device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 
         for (int c = 0; c < QB; c++) {
             u32x4 columns[PAIRS];
 #pragma unroll
-            for (int n = 0; n < PAIRS; n++) {
-                const int at = col + n * 32 + columns_of_lane(g), row = row0 + c * 16 + l16;
-                columns[n] = eight_columns(pair + n, c, bias[n], at, row, row < p.N && at < p.F);
-            }
+            for (int n = 0; n < PAIRS; n++) columns[n] = eight_columns(pair + n, c, bias[n]);
             if constexpr (PAIRS == 2) exchange_8_apart(columns[0], columns[1]);
             uint32_t offset[PAIRS];
 #pragma unroll
@@ -178,17 +178,52 @@ __device__ __forceinline__ void store_blocks(const LinearParams& p, const f32x4 
 }
 template <class T, int PB, int QB>
 __device__ __forceinline__ void linear_store(const LinearParams& p, const f32x4 (&acc)[PB][QB], int col0, int row0, int g, int l16) {
-    with_activation(p.act, [&](auto form) { store_blocks<T, decltype(form)::value, PB, QB>(p, acc, col0, row0, g, l16); });
+    if constexpr (PB > 1) {
+        Residual<PB, QB> residual;
+        load_residual(residual, p, col0, row0, g, l16);
+        with_activation(p.act, [&](auto form) { store_blocks<T, decltype(form)::value, PB, QB>(p, acc, residual, col0, row0, g, l16); });
+    } else {
+        with_activation(p.act, [&](auto form) {           // four columns of a lane at a time
+            constexpr int ACT = decltype(form)::value;
+            const int at = col0 + 4 * g;
+            const u32x2 bias = p.bias ? *reinterpret_cast<const u32x2*>(p.bias + min(at, p.F - 4)) : u32x2{0, 0};
+#pragma unroll
+            for (int c = 0; c < QB; c++) {
+                const int row = row0 + c * 16 + l16;
+                if (row >= p.N || at >= p.F) continue;
+                const u32x2 old = p.residual ? *reinterpret_cast<const u32x2*>(p.residual + (int64_t)row * p.ldr + at) : u32x2{0, 0};
+                const f32x4 v = acc[0][c];
+                *reinterpret_cast<u32x2*>(p.out + (int64_t)row * p.ldo + at) =
+                    u32x2{T::pack(activation<ACT>(v[0] + T::low(bias[0])) + T::low(old[0]), activation<ACT>(v[1] + T::high(bias[0])) + T::high(old[0])),
+                          T::pack(activation<ACT>(v[2] + T::low(bias[1])) + T::low(old[1]), activation<ACT>(v[3] + T::high(bias[1])) + T::high(old[1]))};
+            }
+        });
+    }
 }
 
 // The same for blocks of 32 x 32: a lane holds, of its row (lane % 32), four runs of four columns, 8 i + 4 (lane / 32) on.
 template <class T, int PN, int QN>
 __device__ __forceinline__ void linear_store_32(const LinearParams& p, const f32x16 (&acc)[PN][QN], int col0, int row0, int lane) {
     const int high = lane >> 5;
+    u32x4 residual[4][QN];                               // by 16 columns
+#pragma unroll
+    for (int m = 0; m < 4; m++)
+#pragma unroll
+        for (int c = 0; c < QN; c++) residual[m][c] = u32x4{0, 0, 0, 0};
+    if (p.residual) {
+        const __amdgpu_buffer_rsrc_t from = rows_from(p, p.residual, p.ldr, row0, col0, QN * 32);
+#pragma unroll
+        for (int m = 0; m < 4; m++)
+#pragma unroll
+            for (int c = 0; c < QN; c++) {
+                const int row = c * 32 + (lane & 31), at = m * 16 + 8 * high;
+                residual[m][c] = load_16B(from, row0 + row < p.N && col0 + at < p.F ? (uint32_t)(row * (uint32_t)p.ldr + at) * 2u : kNowhere);
+            }
+    }
     with_activation(p.act, [&](auto form) {
         constexpr int ACT = decltype(form)::value;
         static_assert(PN == 2, "64 columns: rows of whole lines of 128 bytes are stored");
-        const __amdgpu_buffer_rsrc_t to = result_rows(p, row0, col0, QN * 32);
+        const __amdgpu_buffer_rsrc_t to = rows_from(p, p.out, p.ldo, row0, col0, QN * 32);
         u32x2 bias[4][2];                                // of the lane's first run and its second of each 16 columns
 #pragma unroll
         for (int m = 0; m < 4; m++)
@@ -199,14 +234,8 @@ __device__ __forceinline__ void linear_store_32(const LinearParams& p, const f32
             u32x4 columns[4];
 #pragma unroll
             for (int m = 0; m < 4; m++) {
-                const int row = row0 + c * 32 + (lane & 31), at = col0 + m * 16 + 8 * high;
-                u32x2 old[2] = {u32x2{0, 0}, u32x2{0, 0}};
-                if (p.residual) {
-                    u32x4 r = {0, 0, 0, 0};
-                    if (row < p.N && at < p.F) r = *reinterpret_cast<const u32x4*>(p.residual + (int64_t)row * p.ldr + at);
-                    from_columns_32(r, old);
-                }
-                u32x2 result[2];
+                u32x2 old[2], result[2];
+                from_columns_32(residual[m][c], old);
 #pragma unroll
                 for (int i = 0; i < 2; i++)
 #pragma unroll
@@ -625,15 +654,19 @@ __global__ __launch_bounds__(512, 2) void linear_wide_kernel(LinearParams p) {
             for (int c = 0; c < 2; c++) Q0[c][ks] = Q0next[c][ks];
     }
     if (wp == 0) turn();
+    Residual<4, 2> residual[2];                    // of this quadrant and the next
+    auto column = [&](int n) { return p0 + n % 2 * 128 + wp * 64; };
+    auto row = [&](int n) { return q0 + n / 2 * 128 + wq * 32; };
+    load_residual(residual[0], p, column(0), row(0), g, l16);
     wait_all_memory();                             // the transfers past the end have landed before the wave may end
     with_activation(p.act, [&](auto form) {
 #pragma unroll
-        for (int j = 0; j < 2; j++)
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                store_blocks<T, decltype(form)::value, 4, 2>(p, acc[i][j], p0 + i * 128 + wp * 64, q0 + j * 128 + wq * 32, g, l16);
-                asm volatile("" ::: "memory");     // one quadrant behind the other: beside the accumulators there is no room for more
-            }
+        for (int n = 0; n < 4; n++) {
+            if (n < 3) load_residual(residual[(n + 1) % 2], p, column(n + 1), row(n + 1), g, l16);
+            asm volatile("" ::: "memory");         // one quadrant behind the other: beside the accumulators there is no room for more
+            store_blocks<T, decltype(form)::value, 4, 2>(p, acc[n % 2][n / 2], residual[n % 2], column(n), row(n), g, l16);
+            asm volatile("" ::: "memory");
+        }
     });
 }
 
