@@ -3,8 +3,8 @@
 // where the first pairs belong to axis 0 (time), the next to axis 1 (height), the last to axis 2 (width).  The inverse, by the
 // opposite angle, is the gradient of the turn.
 //
-// Bound: memory, 2 E bytes read and 2 E written per row of a head: 4608 tokens x 48 heads x 128 take 21 us (5.3 TB/s), 18 000 x 80 131 us
-// (5.6 TB/s; a large copy reaches 5.2 to 5.8).  An angle belongs to a token and a pair and serves every head,
+// Bound: memory, 2 E bytes read and 2 E written per row of a head: 4608 tokens x 48 heads x 128 take 19.5 us (5.8 TB/s), 18 000 x 80 126 us
+// (5.8 TB/s; a large copy reaches 5.2 to 5.8).  An angle belongs to a token and a pair and serves every head,
 // so a thread keeps the sines of its four (or eight) pairs and walks heads.  An angle is formed in 64 bits: positions go to 2^31, and
 // in 32 bits the angle of position 100 000 is off by 4e-3.  What is left of it after the whole turns, rounded to 32 bits, goes to
 // the sine and cosine instructions, which take turns.
@@ -33,13 +33,16 @@ constexpr int kRopeAhead = 4;    // heads of a thread in flight
 constexpr int kRopeMostHeads = 1 << 16;
 
 // A source beyond the L2s passes them by, and a result beyond the last-level cache passes that by as well.  Measured with the kernel that reads
-// the result: 113 MB 43.9 us, sources past 38.6, results too 43.3; 737 MB 267, 262, 253; 28 MB 19.3, 21.4, 23.5.
+// the result: 113 MB 43.9 us, sources past 38.6, results too 43.3; 737 MB 267, 262, 253; 28 MB 19.3, 21.4, 23.5.  A smaller result of
+// whole lines of 128 bytes is written through the L2s as it comes (12 MB 6.0 us, so 5.2; 57 MB 21.4 and 19.4, in place 21.0 and 17.8, with its
+// reader 38.4 and 36.5; 184 MB 65.3 and 60.3; only 111 MB in place lose, 36.7 and 41.8).
 constexpr int64_t kRopeL2 = 32 << 20, kRopeLastLevel = 256 << 20;
-enum RopePast { kNothing = 0, kSource = 1, kSourceAndResult = 2 };
+enum RopeSource { kThroughCaches, kPastL2 };
+enum RopeResult { kKept, kWrittenThrough, kPastLastLevel };
 
 // A thread's item of a row: ADJACENT pairs (elements 2j, 2j + 1), eight elements that hold four pairs; HALVES (elements j, j +
 // pairs), the eight elements of eight pairs in either half.  Items behind the pairs are copied.
-template <class T, bool HALVES, int PAST>
+template <class T, bool HALVES, int SOURCE, int RESULT>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     constexpr int NP = HALVES ? 8 : 4;
     const int slot = threadIdx.x / p.items, item = threadIdx.x - slot * p.items;
@@ -50,11 +53,13 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     const int64_t e0 = HALVES && !turn ? 2 * p.pairs + (item - turned) * 8 : item * 8, e1 = HALVES && turn ? e0 + p.pairs : e0;
     auto load = [](const uint16_t* at) {
         const u32x4* words = reinterpret_cast<const u32x4*>(at);
-        return PAST >= kSource ? __builtin_nontemporal_load(words) : *words;
+        return SOURCE == kPastL2 ? __builtin_nontemporal_load(words) : *words;
     };
-    auto store = [](uint16_t* at, u32x4 value) {
+    const __amdgpu_buffer_rsrc_t result = raw_buffer(p.out, INT32_MAX);   // (a result that is written through reaches no further)
+    auto store = [&](uint16_t* at, u32x4 value) {
         u32x4* words = reinterpret_cast<u32x4*>(at);
-        if (PAST == kSourceAndResult) __builtin_nontemporal_store(value, words);
+        if (RESULT == kWrittenThrough) __builtin_amdgcn_raw_buffer_store_b128(value, result, (int)((at - p.out) * 2), 0, 16);   // sc1
+        else if (RESULT == kPastLastLevel) __builtin_nontemporal_store(value, words);
         else *words = value;
     };
     const int last_head = min(p.heads, ((int)blockIdx.y + 1) * p.side * p.per);
@@ -105,16 +110,16 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     }
 }
 
-template <class T>
-static void rope_launch(const RopeParams& p, dim3 grid, bool halves, int past, hipStream_t s) {
-    auto go = [&](auto halves_c) {
-        constexpr bool HALVES = decltype(halves_c)::value;
-        if (past == kNothing) rope_kernel<T, HALVES, kNothing><<<grid, kRopeThreads, 0, s>>>(p);
-        else if (past == kSource) rope_kernel<T, HALVES, kSource><<<grid, kRopeThreads, 0, s>>>(p);
-        else rope_kernel<T, HALVES, kSourceAndResult><<<grid, kRopeThreads, 0, s>>>(p);
-    };
-    if (halves) go(std::true_type{});
-    else go(std::false_type{});
+template <class T, bool HALVES>
+static void rope_launch(const RopeParams& p, dim3 grid, int source, int result, hipStream_t s) {
+    auto go = [&](auto source_c, auto result_c) { rope_kernel<T, HALVES, decltype(source_c)::value, decltype(result_c)::value><<<grid, kRopeThreads, 0, s>>>(p); };
+    typedef std::integral_constant<int, kThroughCaches> Near;
+    typedef std::integral_constant<int, kPastL2> Far;
+    typedef std::integral_constant<int, kKept> Kept;
+    typedef std::integral_constant<int, kWrittenThrough> Through;
+    if (result == kPastLastLevel) go(Far{}, std::integral_constant<int, kPastLastLevel>{});   // (then the source is as large)
+    else if (source == kPastL2) result == kKept ? go(Far{}, Kept{}) : go(Far{}, Through{});
+    else result == kKept ? go(Near{}, Kept{}) : go(Near{}, Through{});
 }
 
 }  // namespace chipmunk
@@ -154,8 +159,10 @@ extern "C" int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int6
     const dim3 grid((uint32_t)std::min<int64_t>(groups, (1 << 22) / parts), parts);   // a launch has fewer than 2^32 threads
     const auto s = static_cast<hipStream_t>(stream);
     const int64_t bytes = (int64_t)tokens * heads * E * 2;
-    const int past = bytes > kRopeLastLevel ? kSourceAndResult : bytes > kRopeL2 ? kSource : kNothing;
-    if (dtype == CHIPMUNK_DTYPE_BF16) rope_launch<Bf16>(p, grid, halves != 0, past, s);
-    else rope_launch<Fp16>(p, grid, halves != 0, past, s);
+    const bool whole_lines = (reinterpret_cast<uintptr_t>(out) & 127) == 0 && ((halves ? pairs | (E - 2 * pairs) : E) | out_token_stride | out_head_stride) % 64 == 0;
+    const bool near = (__int128)(tokens - 1) * out_token_stride + (__int128)(heads - 1) * out_head_stride + E <= INT32_MAX / 2;   // a 32-bit offset reaches it all
+    const int source = bytes > kRopeL2 ? kPastL2 : kThroughCaches, result = bytes > kRopeLastLevel ? kPastLastLevel : whole_lines && near ? kWrittenThrough : kKept;
+    if (dtype == CHIPMUNK_DTYPE_BF16) halves ? rope_launch<Bf16, true>(p, grid, source, result, s) : rope_launch<Bf16, false>(p, grid, source, result, s);
+    else halves ? rope_launch<Fp16, true>(p, grid, source, result, s) : rope_launch<Fp16, false>(p, grid, source, result, s);
     return launch_status();
 }

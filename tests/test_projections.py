@@ -282,6 +282,26 @@ def test_rope_inside_wider_rows(cm):
 
 
 @gpu
+def test_rope_results_beyond_32_bits(cm):
+    """Results further apart than an offset of 32 bits reaches, of whole lines and not, and one larger than the last-level cache."""
+    heads, E, axes = 3, 128, (64, 0, 0)
+    freqs = cm.rope_frequencies(axes)
+    wide = torch.empty((18, 1 << 26), dtype=torch.bfloat16, device=DEV)
+    for at in (0, 8):
+        out, x, pos = wide[:, at:at + heads * E].unflatten(1, (heads, E)), _randn((18, heads, E), torch.bfloat16, at), _positions(18, at, 1000)
+        for halves in (False, True):
+            want, off = rope_reference(x, pos, freqs, axes, halves, False)
+            cm.rope(x, pos, freqs, out, axes, halves)
+            assert bool(((out.double() - want).abs() <= off).all())
+    x, pos = _randn((23000, 48, E), torch.bfloat16, 1), _positions(23000, 1, 1000)
+    out = torch.empty_like(x)
+    cm.rope(x, pos, freqs, out, axes)
+    for rows in (slice(0, 200), slice(22900, 23000)):
+        want, off = rope_reference(x[rows], pos[rows], freqs, axes, False, False)
+        assert bool(((out[rows].double() - want).abs() <= off).all())
+
+
+@gpu
 @pytest.mark.parametrize("most", [0, 1, 2 ** 20, 2 ** 31])
 def test_rope_far_positions(cm, most):
     """The angle of a far position keeps its precision: 2^31 positions at one radian each."""
