@@ -819,8 +819,14 @@ static double price_of(Form form, int64_t N, int64_t D, int64_t F) {
 static Form linear_form(int N, int D, int F) {
     if (N <= 16 && F / 16 < kMostTiles) return kFewRows;
     Form best = kSmall;
-    for (int f = 1; f < kForms; f++)
-        if (price_of((Form)f, N, D, F) < price_of(best, N, D, F)) best = (Form)f;
+    double least = price_of(best, N, D, F);
+    for (int f = 1; f < kForms; f++) {
+        const double price = price_of((Form)f, N, D, F);
+        if (price < least) {
+            best = (Form)f;
+            least = price;
+        }
+    }
     return best;
 }
 
