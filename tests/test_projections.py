@@ -178,6 +178,23 @@ def test_linear_beyond_32_bits(cm):
     assert bool(((out.double() - want).abs() <= off).all())
 
 
+@gpu
+@pytest.mark.parametrize("N,D,F", [(30000, 64, 5120), (30000, 512, 5120), (120, 136, 1130048), (190, 264, 720064)])
+def test_linear_results_past_the_caches(cm, N, D, F):
+    """Larger than the last-level cache: of whole lines, and the same in rows that are not."""
+    x, w, bias, residual = _randn((N, D), torch.bfloat16, 1), _randn((F, D), torch.bfloat16, 2, 0.1), _randn((F,), torch.bfloat16, 3), _randn((N, F), torch.bfloat16, 4)
+    out = torch.full((N, F), math.nan, dtype=torch.bfloat16, device=DEV)
+    cm.linear(x, w, bias, residual, out)
+    for rows in (slice(0, 10), slice(N - 10, N)):
+        want, off = linear_reference(x[rows], w, bias, residual[rows], 2)
+        assert bool(((out[rows].double() - want).abs() <= off).all())
+    assert not bool(out.isnan().any())
+    frame, inside = _spread(out, 8, 7.0)
+    inside.fill_(math.nan)
+    cm.linear(x, w, bias, residual, inside)
+    assert torch.equal(inside, out) and bool((frame[:, F:] == 7.0).all())
+
+
 def test_every_form_of_tiles_is_reached(cm):
     """From one row to thousands; the sizes of test_linear take each form."""
     form = cm.load().chipmunk_internal_linear_form
