@@ -276,6 +276,9 @@ __device__ __forceinline__ void wait_steps(int left) {
 // Tiles of 32 PB columns x 32 QB rows.  The contraction goes in steps of 64; TEAMS of four waves (each wave half the columns and
 // half the rows) take the steps in turn, each team through a ring of STAGES stages of its own in LDS, and their sums meet at the
 // end.  A wave holds the operands of a slice (32 of the contraction) ahead, so a stage is free again halfway through its step.
+//
+// Bound: for few tiles the latency of a step, of which STAGES - 1 are on their way; with every CU busy what the CUs can fetch (see
+// linear_block_kernel): 2000 rows, 4096 -> 4096 by 128 x 128 56 us (1.2 PFLOP/s).
 template <class T, int PB, int QB, int STAGES, int TEAMS>
 __global__ __launch_bounds__(256 * TEAMS, 2) void linear_ring_kernel(LinearParams p) {
     constexpr int BP = 32 * PB, BQ = 32 * QB, STAGE = (BP + BQ) * 128;
@@ -398,8 +401,9 @@ __global__ __launch_bounds__(256 * TEAMS, 2) void linear_ring_kernel(LinearParam
 // Tiles of 64 PN columns x 64 QN rows, four waves of half of either, one workgroup to a CU: where that makes one round of tiles, or
 // little more.  One wave per SIMD keeps the matrix pipe full only with products of 32 x 32 (2.01 PFLOP/s; of 16 x 16: 1.52).
 //
-// Bound: a step of 128 x 128 takes 0.36 us on a few CUs, of which its products are 0.25, and 0.55 us where all of them fetch (2.5
-// TB/s of weights; more stages, or waves that fetch nothing but weights or rows, changed nothing).
+// Bound: a step of 128 x 128 takes 0.36 us on a few CUs, of which its products are 0.25, and 0.55 us where all of them fetch: some 90
+// lines of 128 bytes of a CU are outstanding at a time, for 590 cycles each (333 rows, 4096 -> 10 880: 41 us; more stages, or waves that
+// fetch nothing but weights or rows, changed nothing).
 template <class T, int PN, int QN, int STAGES>
 __global__ __launch_bounds__(256, 1) void linear_block_kernel(LinearParams p) {
     typedef typename T::x8 x8;
@@ -515,6 +519,7 @@ __device__ __forceinline__ void finish_products() { asm volatile("s_nop 15\n\ts_
 //     1       P1 (t) and Q0 (step t + 1)   P0 and Q1 (t + 2)              P1 x Q1, P1 x Q0
 // A slot ends with its LDS reads complete and with the wave's share of what the next slot reads landed: all but the eight
 // transfers of the last two slots.  CUT: the contraction's last step is not whole.
+// 75 600 rows, 5120 -> 15 360: 8.47 ms (1.40 PFLOP/s, matrix pipes 80 % busy at 1.76 GHz, the power limit's clock).
 constexpr int kWideHalf = 128 * 128;               // bytes of a half tile
 constexpr int kWideStage = 4 * kWideHalf;
 template <class T, bool CUT>
@@ -674,7 +679,8 @@ __global__ __launch_bounds__(512, 2) void linear_wide_kernel(LinearParams p) {
 // ring of its own, so none waits for another before their sums meet in LDS.
 //
 // Bound: memory, the weights read once.  They pass through LDS because a transfer then fetches whole lines of 128 bytes (eight
-// rows); straight to registers in the product's layout a load fetches 64 bytes of sixteen rows, and a CU got half the rate.
+// rows); straight to registers in the product's layout a load fetches 64 bytes of sixteen rows, and a CU got half the rate.  2 rows, 5120
+// -> 30 720: 52.6 us, 6.0 TB/s.
 template <class T, int CB, int NX, int STAGES>
 __global__ __launch_bounds__(512) void linear_patch_kernel(LinearParams p) {
     typedef typename T::x8 x8;
