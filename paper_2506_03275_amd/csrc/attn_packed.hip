@@ -715,7 +715,11 @@ static int32_t launch_rows(PackedParams p, hipStream_t stream) {
 }
 
 // A few queries over many keys are walked in parts: rows of a key head, keys of a workgroup, parts of the longest sequence.
-// rows 0: in whole sequences.
+// rows 0: in whole sequences, where parts and their joining take longer; over 264 batches, all sequences as long, the choice takes 1.018 times
+// the quicker's time in the mean (us by parts and whole: 8 heads x 4 rows, 1000 keys 8.3 8.0, 1500 8.5
+// 9.7, 4000 10.8 27.6; 128 heads, 1500 24.2 22.8, 2000 29.5 31.5; 8 heads x 64 rows, 2000 15.8 11.5, 8000 19.0 47.0; 128 heads 45 33 and 125 113;
+// 1 head x 512 rows, 2000 15.4 11.3, 8000 19.4 39.5; 8 heads 22.4 15.8, 4000 35 27, 8000 41 47; 32 heads 47 29 and 125 129).  However many the
+// heads, parts begin at 3000 or 5000 keys: whole, the one long sequence of a ragged batch would take one CU a head.
 struct FewPlan {
     int rows, part_keys, parts;
 };
@@ -725,8 +729,9 @@ struct FewPlan {
 // to 4125 keys 42.4 42.9 44.1 62.1 86.4; 16 of 36 258 63.8 58.6 52.1 49.2 64.3; 512 of 10 000, all as long, 514 478 455 444 463).
 static FewPlan few_plan(int S, int Hq, int Hk, int max_q, int max_k) {
     const int64_t rows = (int64_t)max_q * (Hq / Hk), heads = (int64_t)S * Hk;
-    if (max_k <= 1024 || rows > 256 || (rows > 64 && heads * ((rows + 63) / 64) >= 128)) return FewPlan{0, 0, 0};
     const int64_t blocks = heads * ((rows + 63) / 64);
+    const int64_t least_keys = rows <= 32 ? std::min<int64_t>(1000 + 15 * heads, 3000) : std::min<int64_t>(2800 + 30 * blocks, 5000);
+    if (max_k <= least_keys || rows > 1024 || (rows > 32 && blocks >= 128)) return FewPlan{0, 0, 0};
     int keys = 0;
     double least = 0.0;
     for (int length = 256; length <= 4096; length *= 2) {
