@@ -64,7 +64,7 @@ __device__ __forceinline__ i32x4 operand_rows(const uint16_t* base, int64_t ld, 
 }
 constexpr uint32_t kNowhere = 0x80000000u;   // an offset behind every such buffer: the load gives zeros
 
-// Asynchronous 16-byte load to LDS through a buffer, with a wave-uniform part of the offset.  Not a memory access to the compiler,
+// Asynchronous 16-byte load to LDS through a buffer, with a wave-uniform part of the offset, which lies inside the buffer.  Not a memory access to the compiler,
 // so LDS reads of other stages may be scheduled across it; waits and barriers order it against those of its own.
 __device__ __forceinline__ void load_rows_to_lds_16B(i32x4 buffer, uint32_t byte_offset, uint32_t uniform_offset, uint32_t lds_wave_base) {
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
@@ -303,12 +303,13 @@ __global__ __launch_bounds__(256 * TEAMS, 2) void linear_ring_kernel(LinearParam
     for (int n = 0; n < NQ; n++) xoff[n] = (uint32_t)(n * 32 + first_row) * (uint32_t)(p.ldx * 2) + chunk * 16u;
     const int all_chunks = p.D / 8, all_steps = (p.D + 63) / 64, steps = (all_steps + TEAMS - 1) / TEAMS;
     const uint32_t lds0 = lds_address(smem) + (uint32_t)(team * STAGES * STAGE);
-    // transfer n of the team's step t, zeros where the contraction ends
+    // transfer n of the team's step t, zeros where the contraction ends.  (A team may have one step less than the other; in its place the last
+    // step's offset stands, which is inside even a single row: the hardware takes the uniform offset from the buffer's size.)
     auto request = [&](int t, int n) {
-        const int step = t * TEAMS + team;
+        const int step = t * TEAMS + team, inside = TEAMS == 1 ? step : min(step, all_steps - 1);
         const uint32_t to = lds0 + (uint32_t)(t % STAGES * STAGE + (n < NP ? n : n - NP) * 4096 + (n < NP ? 0 : BP * 128) + w * 1024);
         const uint32_t off = step * 8 + chunk < all_chunks ? (n < NP ? woff[n < NP ? n : 0] : xoff[n < NP ? 0 : n - NP]) : kNowhere;
-        load_rows_to_lds_16B(n < NP ? wbuf : xbuf, off, (uint32_t)step * 128u, to);
+        load_rows_to_lds_16B(n < NP ? wbuf : xbuf, off, (uint32_t)inside * 128u, to);
     };
     auto request_all = [&](int t) {
 #pragma unroll

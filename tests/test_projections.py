@@ -96,6 +96,31 @@ def test_linear(cm, N, D, F, dtype):
     _check_linear(cm, N, D, F, dtype, seed // 8 % 4, bias=seed % 3 != 0, residual=seed % 5 != 0, seed=seed)
 
 
+# one row in the last tile of 64 or 128, whose contraction has an odd number of steps, the last one cut: two teams of waves, the second with
+# a step less
+LONE_ROWS = [(257, 3488, 1856), (193, 4400, 2512), (385, 3728, 1976), (513, 936, 2224), (385, 5560, 2960)]
+
+
+def test_lone_rows_take_two_teams(cm):
+    form = cm.load().chipmunk_internal_linear_form
+    assert {form(*size) for size in LONE_ROWS} == {1, 2}
+    assert all(N % (64, 128)[form(N, D, F) - 1] == 1 and D % 64 and -(-D // 64) % 2 for N, D, F in LONE_ROWS)
+
+
+@gpu
+@pytest.mark.parametrize("N,D,F", LONE_ROWS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_a_lone_row_and_a_cut_step(cm, N, D, F, dtype):
+    """Of a tile's only row nothing behind the contraction's end gets into a result: NaN stand there."""
+    x, w = _randn((N, D), dtype, N), _randn((F, D), dtype, D, 1 / math.sqrt(D))
+    frame = torch.full((N * D + 4096,), math.nan, dtype=dtype, device=DEV)
+    frame[:N * D] = x.view(-1)
+    want, off = linear_reference(x, w, None, None, 2)
+    out = torch.full((N, F), math.nan, dtype=dtype, device=DEV)
+    cm.linear(frame[:N * D].view(N, D), w, None, None, out)
+    assert bool(((out.double() - want).abs() <= off).all())
+
+
 @gpu
 @pytest.mark.parametrize("act", [0, 1, 2, 3])
 @pytest.mark.parametrize("bias,residual", [(False, False), (True, False), (False, True), (True, True)])
