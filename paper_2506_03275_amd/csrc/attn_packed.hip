@@ -12,6 +12,7 @@
 #include "element.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace chipmunk {
@@ -702,15 +703,28 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedParams p) {
     }
 }
 
+// Tiles (of a head, or of a sequence and key head) and workgroups of a launch: in double precision, for sizes that no launch covers.
+constexpr double kMostWorkgroups = 1 << 24;               // a launch has fewer than 2^32 threads
+struct PackedGrid {
+    double tiles, workgroups;
+};
+static PackedGrid rows_grid(int rows, int S, int64_t Tq, int Hq, int Hk, int max_q) {
+    const int64_t tiles = max_q <= rows ? S : Tq / rows + std::min<int64_t>(S, Tq);
+    // (whole turns over the XCDs: tiles of every XCD's heads, or of a head's XCDs)
+    const int64_t whole = Hk % 8 != 0 && 8 % Hk == 0 ? (tiles + 8 / Hk - 1) / (8 / Hk) * (8 / Hk) : tiles;
+    return PackedGrid{(double)tiles, (double)whole * Hq};
+}
+static PackedGrid few_grid(int rows, int S, int Hk, int64_t few_rows, int parts) {
+    const double tiles = (double)((few_rows + rows - 1) / rows);
+    return PackedGrid{tiles, tiles * S * Hk * parts};
+}
+
 template <class T, int E, int NQB>
 static int32_t launch_rows(PackedParams p, hipStream_t stream) {
     constexpr int ROWS = 64 * NQB, LDS = 2 * kStepTiles * 2 * kTile * E * 2;
-    const int64_t tiles = p.max_q <= ROWS ? p.S : (int64_t)p.Tq / ROWS + std::min(p.S, p.Tq);
-    // (a grid of whole turns over the XCDs: tiles of every XCD's heads, or of a head's XCDs)
-    const int64_t whole = p.Hk % 8 == 0 ? tiles * p.Hq : 8 % p.Hk == 0 ? (tiles + 8 / p.Hk - 1) / (8 / p.Hk) * 8 * p.G : tiles * p.Hq;
-    if (whole >= INT64_C(1) << 24) return CHIPMUNK_ERR_SHAPE;
-    p.tiles = (int)tiles;
-    attn_packed_rows_kernel<T, E, NQB><<<(uint32_t)whole, 256, LDS, stream>>>(p);
+    const PackedGrid grid = rows_grid(ROWS, p.S, p.Tq, p.Hq, p.Hk, p.max_q);
+    p.tiles = (int)grid.tiles;
+    attn_packed_rows_kernel<T, E, NQB><<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
     return launch_status();
 }
 
@@ -752,7 +766,10 @@ static size_t few_bytes(const FewPlan& f, int S, int Hk, int E) {
 // 64 keys take the workgroup that has the most of them, which bounds a small launch; what 64 rows x 64 keys take where the CUs are full, and a share
 // of the last workgroup.  Fitted to 2567 random batches of 1 to 32 sequences of up to 10 000 tokens, 1 to 120 heads, causal or not: the form
 // taken is 1.010 times the quickest's time in the mean.  The lengths are on the device: one sequence of the given limits is assumed, and the
-// rest of the rows evenly spread over the others.
+// rest of the rows evenly spread over the others.  Workgroups beyond those find nothing to do, which takes 0.8 us for a thousand of them: the
+// rows of a key head are cut as often for every sequence as for the longest (over 1365 batches of one or two prompts of 100 to 8000 tokens and up to
+// 2000 of 1 to 40 1.031 times the quickest's time in the mean; without this term 1.40, and 14.6 at most: 6430 tokens and 483 single ones, 8
+// heads over 1, 64 rows 88 us, 32 rows of the key head 582).
 enum PackedForm { kKeys16, kKeys32, kRows64, kRows128, kRows192, kPackedForms };
 struct PackedPrice {
     int rows;
@@ -761,9 +778,12 @@ struct PackedPrice {
 static const PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.8f, 0.17f, 0.81f}, {32, 6.6f, 0.21f, 0.37f}, {64, 3.2f, 0.80f, 0.36f}, {128, 4.4f, 1.26f, 0.29f}, {192, 9.2f, 1.22f, 0.275f}},
                                                            {{16, 5.5f, 0.165f, 1.78f}, {32, 8.3f, 0.43f, 0.70f}, {64, 5.1f, 0.94f, 0.64f}, {128, 5.1f, 1.49f, 0.50f}, {192, 13.8f, 2.34f, 0.41f}}};
 static const float kPackedLast[2][2] = {{0.35f, 0.25f}, {0.49f, 0.53f}};   // of E = 64, 128; all keys, causal
+static const double kPackedEmpty = 0.0008;               // us
 static double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
     const PackedPrice& f = kPackedPrices[E == 128][form];
     const bool grouped = form <= kKeys32;                 // rows of a key head, of all its queries' heads
+    const double launched = (grouped ? few_grid(f.rows, S, Hk, (int64_t)max_q * (Hq / Hk), 1) : rows_grid(f.rows, S, Tq, Hq, Hk, max_q)).workgroups;
+    if (launched >= kMostWorkgroups) return HUGE_VAL;
     const double per_query = grouped ? (double)Hq / Hk : 1.0, heads = grouped ? Hk : Hq;
     double workgroups = 0, units = 0;
     const double rest = S > 1 ? std::max(0.0, (double)(Tq - max_q) / (S - 1)) : 0.0;
@@ -776,7 +796,7 @@ static double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, i
     add(1, max_q, max_k);
     if (S > 1) add(S - 1, rest, rest * max_k / max_q);
     const double longest = max_k / 64.0, last = kPackedLast[E == 128][causal != 0] * longest * (f.rows / 64.0) * f.full;
-    return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last);
+    return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last) + kPackedEmpty * std::max(0.0, launched - workgroups);
 }
 static PackedForm packed_form(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
     PackedForm best = kKeys16;
@@ -796,10 +816,11 @@ static int32_t launch_few(PackedParams p, hipStream_t stream) {
     constexpr int TOGETHER = NQB < 2 ? NQB : 2;
     constexpr int LDS = std::max(4 * 2 * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
     const auto kernel = attn_packed_few_kernel<T, E, NQB>;
+    const PackedGrid grid = few_grid(16 * NQB, p.S, p.Hk, p.few_rows, p.parts);
+    if (grid.workgroups >= kMostWorkgroups) return CHIPMUNK_ERR_SHAPE;
     if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
-    p.tiles = (p.few_rows + 16 * NQB - 1) / (16 * NQB);
-    if ((int64_t)p.S * p.Hk * p.parts * p.tiles >= INT64_C(1) << 24) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
-    kernel<<<(uint32_t)(p.S * p.Hk * p.parts * p.tiles), 256, LDS, stream>>>(p);
+    p.tiles = (int)grid.tiles;
+    kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
     if (p.parts > 1) attn_packed_join_kernel<T, E><<<(uint32_t)(((int64_t)p.S * p.Hk * p.few_rows + 3) / 4), 256, 0, stream>>>(p);
     return launch_status();
 }
@@ -816,8 +837,8 @@ static int32_t launch_packed(PackedParams p, const FewPlan& few, void* ws, size_
         return few.rows <= 16 ? launch_few<T, E, 1>(p, stream) : few.rows <= 32 ? launch_few<T, E, 2>(p, stream) : launch_few<T, E, 4>(p, stream);
     }
     const PackedForm form = packed_form(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, p.max_k, p.causal);
+    if (packed_price(form, p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, p.max_k, p.causal) == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;   // no form's launch covers it
     if (form <= kKeys32) {
-        if ((int64_t)p.max_q * p.G > INT32_MAX / 2) return CHIPMUNK_ERR_SHAPE;
         p.few_rows = p.max_q * p.G;
         p.part_keys = INT32_MAX;
         p.parts = 1;

@@ -145,6 +145,42 @@ def test_large_batches(cm, E, causal, form, Hq, Hk, lengths):
         assert torch.equal(again, out)
 
 
+# one long prompt among many short sequences, S, Tq, Hq, Hk, E, max_q: forms that cut every sequence like the longest launch workgroups by the
+# million, or more than a launch holds
+RAGGED = [(1024, 5119, 128, 8, 128, 4096), (4096, 5119, 64, 8, 64, 1024), (484, 6913, 8, 1, 64, 6430), (1000, 8194, 96, 12, 128, 2639), (447, 5085, 8, 8, 64, 2676),
+          (20000, 40000, 64, 8, 128, 20001)]
+
+
+def test_one_long_sequence_among_many_short_ones_is_not_cut_a_million_times(cm):
+    form = cm.load().chipmunk_internal_attn_packed_form
+    for S, Tq, Hq, Hk, E, most in RAGGED:
+        for causal in (False, True):
+            taken = form(S, Tq, Hq, Hk, E, most, most, causal)
+            rows = (16, 32, 64, 128, 192)[taken]
+            workgroups = S * Hk * -(-most * (Hq // Hk) // rows) if taken < 2 else (S if most <= rows else Tq // rows + S) * Hq
+            assert workgroups < 2 ** 24
+            # the queries that there are, cut by themselves, and one more tile a sequence and head
+            assert workgroups <= 2 * (Tq // 64 + S) * Hq, (S, Tq, Hq, Hk, E, most, taken, workgroups)
+
+
+@gpu
+@pytest.mark.parametrize("S,Hq,Hk,E,most,at", [(1024, 128, 8, 128, 4096, 0), (4096, 64, 8, 64, 1024, 4095), (447, 8, 8, 64, 2676, 200)])
+def test_one_long_sequence_among_many_short_ones(cm, S, Hq, Hk, E, most, at):
+    lengths = [1] * S
+    lengths[at] = most
+    q, k, v, cu_q, cu_k, _ = _inputs(lengths, lengths, Hq, Hk, E, torch.bfloat16, S, packed=True)
+    out = _run(cm, q, k, v, cu_q, cu_k, None, lengths, lengths, True, E ** -0.5)
+    rows = slice(at, at + most)
+    for h in (0, Hq - 1):
+        g = h // (Hq // Hk)
+        want, off = reference(q[rows, h:h + 1], k[rows, g:g + 1], v[rows, g:g + 1], True, E ** -0.5)
+        assert bool(((out[rows, h:h + 1].double() - want).abs() <= off).all())
+    # a token that sees itself alone takes its value as it is
+    alone = torch.ones(out.shape[0], dtype=torch.bool, device=DEV)
+    alone[rows] = False
+    assert torch.equal(out[alone], v[alone].repeat_interleave(Hq // Hk, 1))
+
+
 CONTINUED = [([5], [70]), ([1], [1]), ([1], [64]), ([1], [65]), ([1, 1, 1], [1, 4000, 129]), ([17, 3], [200, 3]), ([150], [1000]), ([64, 0, 9], [64, 30, 0]),
              ([300, 2], [100, 1]), ([200], [1]), ([4, 4, 4, 4], [4, 5, 600, 0]), ([1] * 40, list(range(0, 2000, 50))), ([130, 1, 33], [129, 900, 31]), ([8], [5000]), ([1], [9001])]
 
