@@ -315,9 +315,10 @@ int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_head_
  *   out[i,h] = softmax_j(softmax_scale * <q[i,h], k[j]>) v[j]     over the keys that are seen; none: zero.
  * Scores, softmax and sums are fp32; a probability is rounded to the element type where it meets v, and so in its sum.  Keys that
  * a query does not see have no influence on it, whatever k and v hold there.
- * q, k, v, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E.  Tq, Tk:
- * rows of q (and out) and of k and v.  Rows of out that belong to no sequence are left as they were.  max_q, max_k: no sequence
- * has more queries, keys; sequences that do are cut there, which gives wrong results.  cu_q, cu_k: [S+1] int32 ascending; with
+ * q, k, v, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E; out
+ * overlaps nothing else.  Tq, Tk: rows of q (and out) and of k and v.  Rows of out that belong to no sequence are left as they were.  max_q, max_k: no sequence
+ * has more queries, keys; sequences that do are cut there, which gives wrong results.  They may be far too large (up to
+ * 2^31 - 1; the work of few queries is divided by max_k, so a close one is quicker).  cu_q, cu_k: [S+1] int32 ascending; with
  * k_len, cu_k[S] is not read.  Entries are clamped so that bad ones give wrong results, not accesses outside the tensors.
  * E in {64,128}; token strides < 2^24; (Tq / 192 + S + 8) * Hq < 2^24.  ws: chipmunk_attn_packed_workspace_bytes() (0: ws may be NULL; also 0 on bad
  * arguments), contents undefined afterwards, not to be shared by calls that may overlap. */

@@ -488,7 +488,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
     // the first keys that the first and the last row do not see
     const int seen_by_all = p.causal ? min(ks.count, row0 / p.G + 1 + past) : ks.count;
     const int seen = p.causal ? min(ks.count, (row0 + rows - 1) / p.G + 1 + past) : ks.count;
-    const int start = part * p.part_keys, end = min(p.parts == 1 ? seen : ks.count, start + p.part_keys);
+    const int start = part * p.part_keys, end = start + min((p.parts == 1 ? seen : ks.count) - start, p.part_keys);   // (no sum passes 31 bits)
     if (start >= end && part > 0) return;                 // (without any key the first part writes zeros)
     const uint16_t* kh = p.k + head * p.k_head + (int64_t)ks.first * p.k_token;
     const uint16_t* vh = p.v + head * p.v_head + (int64_t)ks.first * p.v_token;
@@ -645,7 +645,7 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedParams p) {
     const int row = (int)(id % p.few_rows), head = (int)(id / p.few_rows % p.Hk), s = (int)(id / p.few_rows / p.Hk);
     const Rows qs = queries_of(p, s), ks = keys_of(p, s);
     if (row >= qs.count * p.G || ks.count <= p.part_keys) return;
-    const int parts = (ks.count + p.part_keys - 1) / p.part_keys;
+    const int parts = (ks.count - 1) / p.part_keys + 1;
     const float* sums = p.partial + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * E;
     const float* stats = p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * 2;
     constexpr int PER = E / 64;                           // columns of a lane
@@ -741,22 +741,39 @@ struct FewPlan {
 // one and two workgroups to a CU some CUs have twice the work.  Measured on 112 batches, ragged and not, 1 to 512 heads of 1300 to 38 000
 // keys: the length taken is 1.022 times the quickest's time in the mean, 1.21 at most (us by 256, 512, 1024, 2048, 4096 keys: 136 heads of up
 // to 4125 keys 42.4 42.9 44.1 62.1 86.4; 16 of 36 258 63.8 58.6 52.1 49.2 64.3; 512 of 10 000, all as long, 514 478 455 444 463).
+// A limit may be far above the lengths: beyond 2^17 workgroups the parts grow with it, so that neither the workspace (4.4 GB at most) nor the
+// launch does, and the call goes by the rows that there are (few_plan_within).
+constexpr int64_t kMostPartWorkgroups = 1 << 17;
+static int parts_of(int max_k, int keys) { return (int)(((int64_t)max_k + keys - 1) / keys); }
 static FewPlan few_plan(int S, int Hq, int Hk, int max_q, int max_k) {
     const int64_t rows = (int64_t)max_q * (Hq / Hk), heads = (int64_t)S * Hk;
+    if (rows > 1024 || heads > kMostPartWorkgroups / 2) return FewPlan{0, 0, 0};
     const int64_t blocks = heads * ((rows + 63) / 64);
     const int64_t least_keys = rows <= 32 ? std::min<int64_t>(1000 + 15 * heads, 3000) : std::min<int64_t>(2800 + 30 * blocks, 5000);
-    if (max_k <= least_keys || rows > 1024 || (rows > 32 && blocks >= 128)) return FewPlan{0, 0, 0};
+    if (max_k <= least_keys || (rows > 32 && blocks >= 128)) return FewPlan{0, 0, 0};
     int keys = 0;
     double least = 0.0;
     for (int length = 256; length <= 4096; length *= 2) {
-        const int64_t workgroups = blocks * (((int64_t)max_k + length - 1) / length);
+        const int64_t workgroups = blocks * parts_of(max_k, length);
         const double price = length * (workgroups > 256 && workgroups < 512 ? 1.3 : 1.0) + (double)max_k / length * (30.0 + (double)blocks);
         if (keys == 0 || price < least) {
             keys = length;
             least = price;
         }
     }
-    return FewPlan{(int)rows, keys, (int)(((int64_t)max_k + keys - 1) / keys)};
+    while (blocks * parts_of(max_k, keys) > kMostPartWorkgroups) keys *= 2;   // (two parts of 2^30 keys at the latest)
+    return FewPlan{(int)rows, keys, parts_of(max_k, keys)};
+}
+// The plan for no more than Tk keys, with no more parts than the workspace of the limits as given has room for.
+static FewPlan few_plan_within(int S, int Hq, int Hk, int max_q, int max_k, int Tk) {
+    const FewPlan given = few_plan(S, Hq, Hk, max_q, max_k);
+    if (given.rows == 0 || max_k <= Tk) return given;
+    FewPlan plan = few_plan(S, Hq, Hk, max_q, Tk);
+    while (plan.parts > given.parts) {
+        plan.part_keys *= 2;
+        plan.parts = parts_of(Tk, plan.part_keys);
+    }
+    return plan;
 }
 static size_t few_bytes(const FewPlan& f, int S, int Hk, int E) {
     return f.parts <= 1 ? 0 : (size_t)S * Hk * f.parts * f.rows * (E + 2) * sizeof(float);
@@ -817,7 +834,6 @@ static int32_t launch_few(PackedParams p, hipStream_t stream) {
     constexpr int LDS = std::max(4 * 2 * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
     const auto kernel = attn_packed_few_kernel<T, E, NQB>;
     const PackedGrid grid = few_grid(16 * NQB, p.S, p.Hk, p.few_rows, p.parts);
-    if (grid.workgroups >= kMostWorkgroups) return CHIPMUNK_ERR_SHAPE;
     if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
     p.tiles = (int)grid.tiles;
     kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
@@ -829,7 +845,6 @@ template <class T, int E>
 static int32_t launch_packed(PackedParams p, const FewPlan& few, void* ws, size_t ws_bytes, hipStream_t stream) {
     if (few.rows > 0) {
         if (few_bytes(few, p.S, p.Hk, E) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
-        if ((int64_t)p.S * p.Hk * few.rows >= INT64_C(1) << 26) return CHIPMUNK_ERR_SHAPE;   // a launch has fewer than 2^32 threads
         p.few_rows = few.rows;
         p.part_keys = few.part_keys;
         p.parts = few.parts;
@@ -890,7 +905,7 @@ extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_strid
     const PackedParams p{q, k, v, out, cu_q, cu_k, k_len, q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
                          out_token_stride, out_head_stride, S, Tq, Tk, Hq, Hk, Hq / Hk, std::min(max_q, Tq), std::min(max_k, Tk), causal != 0, 0, 0, 0, 0, nullptr,
                          softmax_scale * 1.4426950408889634f};
-    const FewPlan few = few_plan(S, Hq, Hk, max_q, max_k);   // by the limits as given, like the workspace's size
+    const FewPlan few = few_plan_within(S, Hq, Hk, max_q, max_k, Tk);
     const auto st = static_cast<hipStream_t>(stream);
     if (dtype == CHIPMUNK_DTYPE_BF16) return E == 128 ? launch_packed<Bf16, 128>(p, few, ws, ws_bytes, st) : launch_packed<Bf16, 64>(p, few, ws, ws_bytes, st);
     return E == 128 ? launch_packed<Fp16, 128>(p, few, ws, ws_bytes, st) : launch_packed<Fp16, 64>(p, few, ws, ws_bytes, st);

@@ -288,6 +288,26 @@ def test_longer_limits_than_needed(cm):
             _check(cm, nq, nk, 4, 2, 64, torch.float16, True, max_q=max(nq) * more, max_k=max(nk) * more)
 
 
+def test_the_workspace_of_any_limit_is_bounded(cm):
+    """Up to the largest limits, and as many parts as the limits' plan has; without it the call is refused before anything is launched."""
+    of = cm.attn_packed_workspace_bytes
+    for S, Hq, Hk, max_q in ((1, 8, 8, 1), (32, 32, 8, 1), (1, 64, 1, 16), (512, 32, 8, 1), (4096, 32, 8, 1), (2, 8, 8, 1024), (65536, 8, 8, 5), (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 1)):
+        for max_k in (5001, 131072, 2 ** 24, 2 ** 31 - 1):
+            assert 0 <= of(S, Hq, Hk, 128, max_q, max_k) <= 2 ** 17 * 64 * 130 * 4
+    assert of(32, 32, 8, 128, 1, 2 ** 31 - 1) >= of(32, 32, 8, 128, 1, 131072) > 0
+    assert of(1, 8, 8, 128, 2 ** 31 - 1, 2 ** 31 - 1) == 0
+    a = ctypes.c_void_p(0x1000)
+    for max_k in (20000, 2 ** 31 - 1):
+        assert cm.load().chipmunk_attn_packed(a, 4096, 128, a, 1024, 128, a, 1024, 128, a, 4096, 128, a, a, a, 32, 32, 640000, 32, 8, 128, 1, max_k, 1, 0.1, 0, None, 0, None) == -5
+
+
+@gpu
+@pytest.mark.parametrize("nq,nk,Hq,Hk", [([1] * 31 + [2], [1, 0, 70] + [900] * 28 + [4100], 32, 8), ([1], [9001], 8, 1), ([40, 17], [6000, 5100], 16, 2), ([100, 60], [100, 60], 4, 2)])
+def test_limits_far_above_the_lengths(cm, nq, nk, Hq, Hk):
+    for max_q, max_k in ((None, 2 ** 31 - 1), (None, 2 ** 22), (2 ** 31 - 1, 2 ** 31 - 1)):
+        _check(cm, nq, nk, Hq, Hk, 128, torch.bfloat16, True, seed=len(nq), max_q=max_q, max_k=max_k)
+
+
 @gpu
 def test_heads_of_rows_and_other_strides(cm):
     """[heads, rows, E] and rows inside wider ones, and an output with gaps that stay."""
