@@ -383,9 +383,16 @@ def mlp_dense(x, w1, b1, w2, b2, out, a_cache, c, act):
 # ---- projections, rotary positions, attention over packed sequences ------------------------------------------------------
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_MOST = 2 ** 31 - 1   # the library's sizes are ints of 32 bits, to which ctypes would cut a larger one without a word
 
 
-def _strided(t, dtype, name, dims):
+def _int(n, name):
+    if isinstance(n, int) and not -_MOST - 1 <= n <= _MOST:
+        raise ValueError(f"{name}: {n} does not fit 32 bits")
+    return n
+
+
+def _strided(t, dtype, name, dims, most=_MOST):
     """Pointer of a tensor of so many dimensions whose last one is dense; None for None."""
     if t is None:
         return None
@@ -393,6 +400,8 @@ def _strided(t, dtype, name, dims):
         raise TypeError(f"{name}: expected a torch tensor of {dtype}")
     if t.dim() != dims:
         raise ValueError(f"{name}: must have {dims} dimensions")
+    if max(t.shape) > most:
+        raise ValueError(f"{name}: no size may pass 2^31 - 1")
     if t.device.type != "cuda":
         raise ValueError(f"{name}: must live on the GPU")
     if t.device.index != _device():
@@ -424,7 +433,7 @@ def linear(x, w, bias, residual, out, act=ACT_NONE):
     if tuple(out.shape) != (N, F) or (residual is not None and residual.shape != out.shape) or (bias is not None and bias.shape[0] != F):
         raise ValueError("out and residual must be [rows of x, rows of w], bias [rows of w]")
     _check(load().chipmunk_linear(px, x.stride(0), pw, pb, pr, 0 if residual is None else residual.stride(0), po, out.stride(0), N, D, F,
-                                  int(act), number, _stream()), "chipmunk_linear")
+                                  _int(int(act), "act"), number, _stream()), "chipmunk_linear")
 
 
 def rope_frequencies(axes, theta=10000.0, device="cuda"):
@@ -443,7 +452,7 @@ def rope(x, pos, freqs, out, axes, halves=False, inverse=False):
     px, po = _strided(x, dtype, "x", 3), _strided(out, dtype, "out", 3)
     pp, pf = _strided(pos, torch.int32, "pos", 2), _strided(freqs, torch.float64, "freqs", 1)
     tokens, heads, E = x.shape
-    t, h, w = axes
+    t, h, w = (_int(n, "axes") for n in axes)
     if out.shape != x.shape:
         raise ValueError("out must have the shape of x")
     if tuple(pos.shape) != (tokens, 3) or not pos.is_contiguous() or freqs.shape[0] != t + h + w:
@@ -453,7 +462,8 @@ def rope(x, pos, freqs, out, axes, halves=False, inverse=False):
 
 
 def attn_packed_workspace_bytes(S, Hq, Hk, E, max_q, max_k):
-    return int(load().chipmunk_attn_packed_workspace_bytes(S, Hq, Hk, E, max_q, max_k))
+    sizes = dict(S=S, Hq=Hq, Hk=Hk, E=E, max_q=max_q, max_k=max_k)
+    return int(load().chipmunk_attn_packed_workspace_bytes(*(_int(n, name) for name, n in sizes.items())))
 
 
 def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k_len=None, ws=None):
@@ -467,7 +477,7 @@ def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k
     i32 = torch.int32
     pq, pk, pv, po = (_strided(t, dtype, name, 3) for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out")))
     pcq, pck, pkl = _strided(cu_q, i32, "cu_q", 1), _strided(cu_k, i32, "cu_k", 1), _strided(k_len, i32, "k_len", 1)
-    pws = _strided(ws, torch.uint8, "ws", 1)
+    pws = _strided(ws, torch.uint8, "ws", 1, most=2 ** 63 - 1)
     (Tq, Hq, E), (Tk, Hk, _), S = q.shape, k.shape, cu_q.shape[0] - 1
     if out.shape != q.shape or k.shape != v.shape or k.shape[2] != E:
         raise ValueError("out must have the shape of q, v that of k, and all the same E")
@@ -475,5 +485,5 @@ def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k
         raise ValueError("cu_q and cu_k must be [sequences + 1], k_len [sequences]")
     strides = [s for t in (q, k, v, out) for s in (t.stride(0), t.stride(1))]
     _check(load().chipmunk_attn_packed(pq, strides[0], strides[1], pk, strides[2], strides[3], pv, strides[4], strides[5], po, strides[6], strides[7],
-                                       pcq, pck, pkl, S, Tq, Tk, Hq, Hk, E, max_q, max_k, int(bool(causal)), float(softmax_scale), number,
+                                       pcq, pck, pkl, S, Tq, Tk, Hq, Hk, E, _int(max_q, "max_q"), _int(max_k, "max_k"), int(bool(causal)), float(softmax_scale), number,
                                        pws, 0 if ws is None else ws.numel(), _stream()), "chipmunk_attn_packed")

@@ -75,3 +75,47 @@ def test_the_binding_does_what_the_python_functions_do(cm, name, dtype):
         assert type(got) is type(want) and (got == want if isinstance(got, tuple) else torch.equal(got, want)), (i, got, want)
         refused += isinstance(got, tuple)
     assert refused >= 4 * len(args)
+
+
+def test_sizes_beyond_32_bits_are_refused(cm):
+    """Not cut to what 32 bits hold, in which more than 2^32 rows would be a few.  (Tensors without memory: the sizes are looked at first.)"""
+    bf, far = torch.bfloat16, 2 ** 32 + 8
+    e = lambda *shape, dtype=bf: torch.empty(shape, dtype=dtype, device="meta")   # noqa: E731
+    cu, heads = e(2, dtype=torch.int32), e(8, 1, 64)
+    for fast in (cm._fast, cm._Python()):
+        before, cm._fast = cm._fast, fast
+        try:
+            for name, args in (("linear", (e(far, 64), e(16, 64), None, None, e(far, 16))),
+                               ("rope", (e(far, 1, 64), e(far, 3, dtype=torch.int32), e(32, dtype=torch.float64), e(far, 1, 64), (32, 0, 0))),
+                               ("attn_packed", (e(far, 1, 64), heads, heads, cu, cu, e(far, 1, 64), 1, 1, True, 0.1))):
+                with pytest.raises(ValueError, match="2\\^31"):
+                    getattr(cm, name)(*args)
+        finally:
+            cm._fast = before
+    for i in range(6):
+        with pytest.raises(ValueError, match="32 bits"):
+            cm.attn_packed_workspace_bytes(*[far if n == i else 64 for n in range(6)])
+
+
+@pytest.mark.gpu
+def test_numbers_beyond_32_bits_are_refused(cm):
+    far = 2 ** 32
+    linear, rope, attn = (_calls("cuda")[name] for name in ("linear", "rope", "attn_packed"))
+    wrong = [("linear", linear[:5] + [far + 1]), ("rope", rope[:4] + [[far + 16, 8, 8 - far], False, True])]
+    wrong += [("attn_packed", attn[:i] + [far + attn[i]] + attn[i + 1:]) for i in (6, 7)]
+    for name, args in wrong:
+        for fast in (cm._fast, cm._Python()):
+            got = _outcome(cm, fast, name, args)
+            assert isinstance(got, tuple) and got[0] == "ValueError" and "32 bits" in got[1], (name, got)
+    many = lambda t: t[:1].expand(far + 8, *t.shape[1:])   # noqa: E731
+    for name, args in (("linear", linear[:1] + [many(linear[1])] + linear[2:]), ("attn_packed", attn[:1] + [many(attn[1]), many(attn[2])] + attn[3:])):
+        for fast in (cm._fast, cm._Python()):
+            got = _outcome(cm, fast, name, args)
+            assert isinstance(got, tuple) and got[0] == "ValueError" and "2^31" in got[1], (name, got)
+
+
+@pytest.mark.gpu
+def test_a_workspace_may_be_larger(cm):
+    args = _calls("cuda")["attn_packed"]
+    large = args[:11] + [torch.empty(2 ** 31 + 64, dtype=torch.uint8, device="cuda")]
+    assert torch.equal(_outcome(cm, cm._fast, "attn_packed", large), _outcome(cm, cm._fast, "attn_packed", args))
