@@ -290,7 +290,8 @@ int32_t chipmunk_mlp_dense(const uint16_t* x, const uint16_t* w1, const uint16_t
  * (same pointer and stride) and overlaps nothing else.  The values between a
  * row's end and the next row are neither read nor written.  D and F multiples
  * of 8, D < 2^20, row strides < 2^22, out fewer than 2^22 tiles of 256 x 256.
- * silu(y) = y / (1 + exp(-y)). */
+ * silu(y) = y / (1 + exp(-y)).  Infinities and NaN go through as the formulas
+ * have it: of minus infinity GELU (both) and silu make NaN, none of them zero. */
 int32_t chipmunk_linear(const uint16_t* x, int64_t ldx, const uint16_t* w, const uint16_t* bias,
                         const uint16_t* residual, int64_t ldr, uint16_t* out, int64_t ldo,
                         int N, int D, int F, int act, int dtype, void* stream);

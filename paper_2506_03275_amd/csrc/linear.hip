@@ -26,11 +26,12 @@ struct LinearParams {
 template <int ACT>
 __device__ __forceinline__ float activation(float y) {
     // x (1 + erf(x / sqrt 2)) / 2 = max(x, 0) - |x| h(|x|), h(z) = erfc(z / sqrt 2) / 2 = exp(-z^2 / 2) t P(t) with t = 1 / (1 + 0.362 z).
-    // P was fitted here to the least relative error, 7.6e-7 over all z; with the rounding of 32 bits the result is off by 2.4e-7 at
-    // most.  With erff, two branches that a wave mostly takes both, the results cost more than the product: 2148 rows, 256 -> 8192,
-    // 53.6 us, now 31.7 (no activation: 22.8).  The bound on |x| keeps an infinite one from 0 times infinity.
+    // P was fitted here to the least relative error, 7.9e-7 for z up to 14 (2.4e-6 at 15, where the exponential leaves 32 bits: zero);
+    // with the rounding of 32 bits the result is off by 2.4e-7 at most.  With erff, two branches that a wave mostly takes both, the
+    // results cost more than the product: 2148 rows, 256 -> 8192, 53.6 us, now 31.7 (no activation: 22.8).  The bound on x keeps infinity
+    // from 0 times infinity; minus infinity is to have it, as in the formula, which gives NaN there, and the other activations' too.
     if constexpr (ACT == CHIPMUNK_ACT_GELU_ERF) {
-        const float z = fminf(fabsf(y), 30.f), t = __builtin_amdgcn_rcpf(__builtin_fmaf(z, 0.362f, 1.f));
+        const float z = fmaxf(fminf(y, 30.f), -y), t = __builtin_amdgcn_rcpf(__builtin_fmaf(z, 0.362f, 1.f));
         float h = 0.047938276f;
         h = __builtin_fmaf(h, t, -0.18000965f);
         h = __builtin_fmaf(h, t, 0.17661723f);

@@ -155,6 +155,28 @@ def test_linear_infinite_and_nan(cm, N):
 
 
 @gpu
+@pytest.mark.parametrize("act", [0, 1, 2, 3])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [1, 12, 40, 300, 3000])
+def test_linear_activations_of_anything(cm, N, act, dtype):
+    """Infinities, NaN and values where an exponential over- or underflows, as the formulas in 64 bits have them: the product is zero, so that
+    the bias goes through the activation as it is."""
+    most = float(torch.finfo(dtype).max)
+    values = [math.inf, -math.inf, math.nan, most, -most, most / 2, -most / 2, 1000.0, -1000.0, 88.0, -88.0, -103.0, 30.0, -30.0, -31.0, 14.0, -14.0, -13.0, 5.0, -5.0, 1.0, -1.0, 0.0, 2.0 ** -14]
+    bias = torch.tensor(values * 11, dtype=dtype, device=DEV)
+    x, w = torch.zeros((N, 72), dtype=dtype, device=DEV), _randn((len(bias), 72), dtype, 3)
+    out = torch.zeros((N, len(bias)), dtype=dtype, device=DEV)
+    cm.linear(x, w, bias, None, out, act)
+    want = _activation(bias.double(), act).expand(N, -1)
+    finite = want.isfinite()
+    assert torch.equal(out.isnan(), want.isnan()) and bool((out[want.isinf()].double() == want[want.isinf()]).all())
+    # as linear_reference has it, without the product: a few units of 32 bits, and the rounding
+    info = torch.finfo(dtype)
+    off = (2e-6 * (1 + want.abs()) if act != 2 else 0) + info.eps / 2 * want.abs() + info.tiny * info.eps
+    assert bool(((out.double() - want).abs() <= off)[finite].all())
+
+
+@gpu
 def test_linear_overflow_is_infinite(cm):
     for dtype, large in ((torch.float16, 200.0), (torch.bfloat16, 1e19)):
         x, w = torch.full((3, 64), large, dtype=dtype, device=DEV), torch.full((16, 64), large, dtype=dtype, device=DEV)
