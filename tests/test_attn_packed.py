@@ -203,6 +203,67 @@ def test_few_queries(cm, nq, G):
     _check(cm, [nq, nq, 1], [700, nq, 2111], 2 * G, 2, 64, torch.float16, True, seed=G)
 
 
+# more than 32 rows of a key head over keys in parts, whose blocks of 16 rows and tiles of 64 go to the workspace and are joined: nq, nk, Hq, Hk
+DIVIDED = [([40, 17], [6000, 5100], 16, 2), ([100], [7001], 8, 1), ([64, 0, 3], [5003, 4790, 4800], 32, 2), ([5, 200], [3000, 5900], 5, 1), ([33], [4097], 1, 1), ([9, 9, 1], [4400, 8, 4000], 16, 4)]
+FAR = [(8, 1, 200000), (3, 3, 140001)]   # one token over more than 64 parts: Hq, Hk, n_k
+
+
+def test_the_batches_are_divided(cm):
+    form = cm.load().chipmunk_internal_attn_packed_form
+    for nq, nk, Hq, Hk in DIVIDED:
+        keys = form(len(nq), sum(nq), Hq, Hk, 128, max(nq), max(nk), 1)
+        assert 32 < max(nq) * (Hq // Hk) <= 1024 and 256 <= keys < max(nk)
+    assert all(form(1, 1, Hq, Hk, 128, 1, nk, 1) >= 256 and -(-nk // form(1, 1, Hq, Hk, 128, 1, nk, 1)) > 64 for Hq, Hk, nk in FAR)
+
+
+@gpu
+@pytest.mark.parametrize("nq,nk,Hq,Hk", DIVIDED)
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_rows_over_divided_keys(cm, nq, nk, Hq, Hk, causal):
+    for dtype, E in ((torch.bfloat16, 128), (torch.float16, 64), (torch.bfloat16, 64), (torch.float16, 128)):
+        for slot in (0, max(nk) + 3):
+            _check(cm, nq, nk, Hq, Hk, E, dtype, causal, seed=E + max(nq), slot=slot)
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk,nk", FAR)
+@pytest.mark.parametrize("sign", [-1.0, 0.0, 1.0])
+def test_a_token_over_more_than_64_parts(cm, Hq, Hk, nk, sign):
+    """Scores that rise or fall from the first part to the last, so that a later round of the joining raises what it holds, or does not."""
+    for dtype, E in ((torch.bfloat16, 128), (torch.float16, 64)):
+        q, k, v, cu_q, cu_k, _ = _inputs([1], [nk], Hq, Hk, E, dtype, 11)
+        q.fill_(0.5)
+        k.copy_((k.float() * 0.1 + sign * torch.linspace(-10, 10, nk, device=DEV)[:, None, None] / math.sqrt(E)).to(dtype))
+        out = _run(cm, q, k, v, cu_q, cu_k, None, [1], [nk], True, 1 / math.sqrt(E))
+        want, off = reference(q, k, v, True, 1 / math.sqrt(E))
+        assert bool(((out.double() - want).abs() <= off).all())
+
+
+@gpu
+@pytest.mark.parametrize("nq,nk,Hq,Hk", [([5], [6000], 4, 2), ([1, 2], [200000, 300], 8, 1), ([100], [7000], 8, 1), ([40, 17], [6000, 5100], 16, 2)])
+@pytest.mark.parametrize("kind", [math.nan, math.inf, -math.inf])
+def test_hidden_keys_of_divided_sequences(cm, nq, nk, Hq, Hk, kind):
+    """As test_hidden_keys_have_no_influence, with the key in the first, a middle or the last part."""
+    for dtype, E in ((torch.bfloat16, 128), (torch.float16, 64)):
+        q, k, v, cu_q, cu_k, _ = _inputs(nq, nk, Hq, Hk, E, dtype, 6)
+        clean = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1)
+        for at in (3, nk[0] // 2, nk[0] - nq[0] // 2 - 1):
+            sees = (torch.arange(nq[0], device=DEV) + nk[0] - nq[0]) >= at
+            for spoiled in (k, v):
+                before = spoiled[at].clone()
+                spoiled[at, :, 5] = kind
+                out = _run(cm, q, k, v, cu_q, cu_k, None, nq, nk, True, 0.1)
+                spoiled[at] = before
+                assert torch.equal(out[:nq[0]][~sees], clean[:nq[0]][~sees]) and torch.equal(out[nq[0]:], clean[nq[0]:])
+                if spoiled is v:
+                    others = [e for e in range(E) if e != 5]
+                    assert torch.equal(out[..., others], clean[..., others])
+                    seen = out[:nq[0]][sees][..., 5]
+                    assert bool(seen.isnan().all() if math.isnan(kind) else (seen == kind).all())
+                elif math.isnan(kind):
+                    assert bool(out[:nq[0]][sees].isnan().all())
+
+
 @gpu
 @pytest.mark.parametrize("scale,size", [(3.0, 1.0), (1e-4, 1.0), (0.125, 30.0), (1.0, 0.01)])
 @pytest.mark.parametrize("E", [64, 128])
