@@ -403,9 +403,9 @@ __global__ __launch_bounds__(256 * TEAMS, 2) void linear_ring_kernel(LinearParam
 // Tiles of 64 PN columns x 64 QN rows, four waves of half of either, one workgroup to a CU: where that makes one round of tiles, or
 // little more.  One wave per SIMD keeps the matrix pipe full only with products of 32 x 32 (2.01 PFLOP/s; of 16 x 16: 1.52).
 //
-// Bound: a step of 128 x 128 takes 0.36 us on a few CUs, of which its products are 0.25, and 0.55 us where all of them fetch: some 90
-// lines of 128 bytes of a CU are outstanding at a time, for 590 cycles each (333 rows, 4096 -> 10 880: 41 us; more stages, or waves that
-// fetch nothing but weights or rows, changed nothing).
+// Bound: a step of 128 x 128 takes 0.36 us on a few CUs, of which its products are 0.25, and 0.55 us where all of them fetch: a CU has 60
+// lines of 128 bytes in flight in the mean, for 340 cycles each, which is 23 bytes a clock, a third of them from beyond the L2 (333 rows, 4096 -> 10 880:
+// 41 us; more stages, or waves that fetch nothing but weights or rows, changed nothing).
 template <class T, int PN, int QN, int STAGES>
 __global__ __launch_bounds__(256, 1) void linear_block_kernel(LinearParams p) {
     typedef typename T::x8 x8;
@@ -521,7 +521,7 @@ __device__ __forceinline__ void finish_products() { asm volatile("s_nop 15\n\ts_
 //     1       P1 (t) and Q0 (step t + 1)   P0 and Q1 (t + 2)              P1 x Q1, P1 x Q0
 // A slot ends with its LDS reads complete and with the wave's share of what the next slot reads landed: all but the eight
 // transfers of the last two slots.  CUT: the contraction's last step is not whole.
-// 75 600 rows, 5120 -> 15 360: 8.47 ms (1.40 PFLOP/s, matrix pipes 80 % busy at 1.76 GHz, the power limit's clock).
+// 75 600 rows, 5120 -> 15 360: 8.44 ms (1.41 PFLOP/s, matrix pipes 78 % busy at 1.79 GHz, the power limit's clock).
 constexpr int kWideHalf = 128 * 128;               // bytes of a half tile
 constexpr int kWideStage = 4 * kWideHalf;
 template <class T, bool CUT>

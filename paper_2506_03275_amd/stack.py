@@ -12,8 +12,8 @@ and weights) runs on a second stream beside the current block's attention and ML
 over.  In a real DiT the next block's input depends on this block's output, so that overlap is a property of a stack
 with pre-generated inputs; what carries over to a model is that the index work needs no result of the delta kernels.
 
-AttentionLayer is the attention half of a block with its projections, for sequences packed one behind the other: a text
-encoder over prompts of different lengths, images of different sizes, or single tokens over what their caches hold.
+AttentionLayer is attention with its projections and residual, without norms and gates, for sequences packed one behind the other: a
+text encoder over prompts of different lengths, images of different sizes, or single tokens over what their caches hold.
 """
 import math
 
