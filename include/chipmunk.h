@@ -321,7 +321,7 @@ int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_head_
  * has more queries, keys; sequences that do are cut there, which gives wrong results.  They may be far too large (up to
  * 2^31 - 1; the work of few queries is divided by max_k, so a close one is quicker).  cu_q, cu_k: [S+1] int32 ascending; with
  * k_len, cu_k[S] is not read.  Entries are clamped so that bad ones give wrong results, not accesses outside the tensors.
- * E in {64,128}; token strides < 2^24; (Tq / 192 + S + 8) * Hq < 2^24.  ws: chipmunk_attn_packed_workspace_bytes() (0: ws may be NULL; also 0 on bad
+ * E in {64,128}; softmax_scale in (0, 2^127]; token strides < 2^24; (Tq / 192 + S + 8) * Hq < 2^24.  ws: chipmunk_attn_packed_workspace_bytes() (0: ws may be NULL; also 0 on bad
  * arguments), contents undefined afterwards, not to be shared by calls that may overlap. */
 size_t chipmunk_attn_packed_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k);
 int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride,

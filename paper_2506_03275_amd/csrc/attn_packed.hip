@@ -31,7 +31,7 @@ struct PackedParams {
     int tiles;     // of one head: as many as there can be
     int part_keys, parts;   // few queries: keys that a workgroup walks, and how many such parts the longest sequence can have
     int few_rows;  // rows of a key head: max_q * G
-    float* partial;         // [S][Hk][parts][few_rows][E] sums, then [S][Hk][parts][few_rows][2]: reference (log2 units), sum of weights
+    float* partial;         // [S][Hk][parts][few_rows][E] sums, then [S][Hk][parts][few_rows][2]: reference (units of <q, k>), sum of weights
     float sl2;     // softmax_scale * log2(e)
 };
 
@@ -594,7 +594,8 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
             const int qb = qb0 + b;
 #pragma unroll
             for (int eb = 0; eb < E / 16; eb++) sums[((w * TOGETHER + b) * (E / 16) + eb) * 64 + lane] = st.O[eb][qb];
-            const float m = st.L[qb][0] == 0.f ? -INFINITY : -st.negm[qb][0] * p.sl2;   // no weight: no reference
+            // (not yet times the scale: a difference of two references times the scale may overflow to a weight of zero, either alone to a NaN)
+            const float m = st.L[qb][0] == 0.f ? -INFINITY : -st.negm[qb][0];   // no weight: no reference
             stats[(w * TOGETHER + b) * 64 + lane] = f32x2{m, st.L[qb][0]};
         }
         lds_accesses_then_barrier();
@@ -612,7 +613,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_packed_few_kernel(
             float total = 0.f;
 #pragma unroll
             for (int v = 0; v < 4; v++) {
-                m[v] = m[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[v] - top);
+                m[v] = m[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[v] - top) * p.sl2);
                 total += l[v] * m[v];
             }
             f32x4 o[COLUMNS];
@@ -661,8 +662,8 @@ __global__ __launch_bounds__(256) void attn_packed_join_kernel(PackedParams p) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
         most = fmaxf(most, top);
-        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most);
-        const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[0] - most);
+        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - most) * p.sl2);
+        const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[0] - most) * p.sl2);
         float add = mine[1] * weight;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
@@ -893,7 +894,8 @@ extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_strid
                                         void* ws, size_t ws_bytes, void* stream) {
     if (!q || !k || !v || !out || !cu_q || !cu_k) return CHIPMUNK_ERR_NULL;
     if (S <= 0 || Tq <= 0 || Tk <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || max_q <= 0 || max_k <= 0) return CHIPMUNK_ERR_SHAPE;
-    if (!is_positive_finite_scalar(softmax_scale)) return CHIPMUNK_ERR_SHAPE;
+    const float sl2 = softmax_scale * 1.4426950408889634f;
+    if (!is_positive_finite_scalar(softmax_scale) || !is_finite_scalar(sl2)) return CHIPMUNK_ERR_SHAPE;
     if ((E != 64 && E != 128) || (dtype != CHIPMUNK_DTYPE_BF16 && dtype != CHIPMUNK_DTYPE_FP16)) return CHIPMUNK_ERR_UNSUPPORTED;
     constexpr int64_t kMostStride = 1 << 24;
     if (Tq == 1) q_token_stride = out_token_stride = E;   // of one row alone a stride means nothing
@@ -908,7 +910,7 @@ extern "C" int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_strid
         return CHIPMUNK_ERR_ALIGN;
     const PackedParams p{q, k, v, out, cu_q, cu_k, k_len, q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
                          out_token_stride, out_head_stride, S, Tq, Tk, Hq, Hk, Hq / Hk, std::min(max_q, Tq), std::min(max_k, Tk), causal != 0, 0, 0, 0, 0, nullptr,
-                         softmax_scale * 1.4426950408889634f};
+                         sl2};
     const FewPlan few = few_plan_within(S, Hq, Hk, max_q, max_k, Tk);
     const auto st = static_cast<hipStream_t>(stream);
     if (dtype == CHIPMUNK_DTYPE_BF16) return E == 128 ? launch_packed<Bf16, 128>(p, few, ws, ws_bytes, st) : launch_packed<Bf16, 64>(p, few, ws, ws_bytes, st);

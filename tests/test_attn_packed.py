@@ -440,7 +440,38 @@ def test_bad_starts_stay_inside(cm):
     assert bool((frame[:20] == 5).all()) and bool((frame[100:] == 5).all())
 
 
+@gpu
+def test_the_largest_and_smallest_scales(cm):
+    """The largest score alone, or all keys alike."""
+    q, k, v, cu_q, cu_k, _ = _inputs([70], [70], 2, 1, 64, torch.bfloat16, 2)
+    scores = (q.double().transpose(0, 1) @ k.double().permute(1, 2, 0))
+    first = scores.argmax(-1)                                                        # [heads, queries]
+    out = _run(cm, q, k, v, cu_q, cu_k, None, [70], [70], False, 2.0 ** 127)
+    assert torch.equal(out, v[:, 0][first].transpose(0, 1))
+    out = _run(cm, q, k, v, cu_q, cu_k, None, [70], [70], False, 2.0 ** -140)
+    want, off = reference(q, k, v, False, 2.0 ** -140)
+    assert bool(((out.double() - want).abs() <= off).all())
+
+
+@gpu
+@pytest.mark.parametrize("n,nk,Hq,Hk", [(130, 130, 40, 40), (1, 9001, 8, 1), (100, 7001, 8, 1), (1503, 1503, 64, 8)])
+def test_the_largest_scale_in_every_form(cm, n, nk, Hq, Hk):
+    """The largest score alone, but for rows whose two largest are closer than what 32 bits tell apart (2^-24 of sums of 64 products)."""
+    q, k, v, cu_q, cu_k, _ = _inputs([n], [nk], Hq, Hk, 64, torch.bfloat16, 3)
+    out = _run(cm, q, k, v, cu_q, cu_k, None, [n], [nk], False, 2.0 ** 127)
+    for h in range(0, Hq, 7):
+        two = (q[:, h].double() @ k[:, h // (Hq // Hk)].double().t()).topk(2, -1)
+        clear = two.values[:, 0] - two.values[:, 1] > 1e-3
+        assert torch.equal(out[clear, h], v[two.indices[clear, 0], h // (Hq // Hk)]) and bool(clear.any())
+
+
 # ---- refusals (no GPU) ------------------------------------------------------------------------------------------------------
+
+def test_refuses_a_scale_that_overflows(cm):
+    a = ctypes.c_void_p(0x1000)
+    for scale in (2.0 ** 128 / 1.44, 3.4e38):
+        assert cm.load().chipmunk_attn_packed(a, 512, 64, a, 256, 64, a, 256, 64, a, 512, 64, a, a, None, 2, 100, 100, 8, 4, 64, 100, 100, 1, scale, 0, a, 1 << 30, None) == -2
+
 
 def test_refuses(cm):
     f, a = cm.load().chipmunk_attn_packed, ctypes.c_void_p(0x1000)
