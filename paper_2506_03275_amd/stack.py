@@ -170,7 +170,9 @@ class AttentionLayer:
     def step(self, x, pos, cu_q, rows, k_len, buffers):
         """x: [tokens, D], the slots' sequences one behind the other (cu_q int32 [slots + 1], a slot without new tokens has
         none); pos: int32 [tokens, 3]; rows: int64 [tokens], each token's row of the caches (slot * slot_tokens + its place);
-        k_len: int32 [slots], tokens of each slot, the new ones among them.  Returns buffers["out"]."""
+        k_len: int32 [slots], tokens of each slot, the new ones among them.  Tokens behind cu_q's last entry (a padded batch) have no
+        influence on the others and results without meaning; their rows of the caches are written, so they need places that no slot has in
+        use.  Returns buffers["out"]."""
         b, H, Hk = buffers, self.heads, self.kv_heads
         qkv = b["qkv"]
         linear(x, self.w_qkv, self.b_qkv, None, qkv.view(qkv.shape[0], -1))

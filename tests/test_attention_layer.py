@@ -118,3 +118,22 @@ def test_captured_steps():
             torch.cuda.synchronize()
             got = call[-1]["out"].clone()
             assert torch.equal(layer.step(*call[:-1], layer.buffers(call[0].shape[0], 2, slot)), got) and bool(got.isfinite().all())
+
+
+def test_a_padded_batch():
+    """Tokens behind the last sequence, whatever they hold, change nothing of the others."""
+    D, heads, kv_heads, E, slot, real, padded = 256, 4, 2, 64, 200, 71, 96
+    layer, r = _layer(torch.bfloat16, D, heads, kv_heads, E, 3, slot, True)
+    new = [40, 0, 31]
+    cu, rows, k_len = _batch(new, [0, 0, 0], slot)
+    x, pos = r(padded, D), torch.randint(0, 50, (padded, 3), dtype=torch.int32, device=DEV)
+    free = torch.arange(3 * slot - (padded - real), 3 * slot, device=DEV)       # the last slot's end
+    results = []
+    for fill in (0.0, 5.0, math.nan):
+        layer.k_cache.fill_(math.nan)
+        layer.v_cache.fill_(math.nan)
+        x[real:] = fill
+        buffers = layer.buffers(padded, 64, slot)
+        buffers["att"].fill_(math.nan)
+        results.append(layer.step(x, pos, cu, torch.cat([rows, free]), k_len, buffers)[:real].clone())
+    assert bool(results[0].isfinite().all()) and all(torch.equal(a, results[0]) for a in results[1:])
