@@ -143,13 +143,18 @@ def _prepare_norm(case, seed):
     return dict(case=case, axes=axes, x=x[:, :H], pos=pos.to(I32).contiguous(), freqs=freqs, out=result(), w=weights, grad=grad, dw=torch.empty((2, E), dtype=F32, device=DEV))
 
 
+def _power(k):
+    """2^k, k from -126 to 127, exactly (a library's powers need not be)."""
+    return ((k + 127) << 23).view(F32)
+
+
 def _e4m3(x):
     """Rows of e4m3 and the exponents of their powers of two, as bytes: x is about code * 2^(byte - 127)."""
     most = x.abs().amax(-1, keepdim=True).float()
     fraction, exponent = torch.frexp(most)                                   # 0.5 <= fraction < 1
     k = (exponent - 9 + (fraction > 0.875).int()).clamp(-126, 127)
     k = torch.where(most > 0, k, 0)
-    return torch.ldexp(x.float(), -k).to(torch.float8_e4m3fn), (k + 127).to(U8)[..., 0]
+    return (x.float() * _power(-k)).to(torch.float8_e4m3fn), (k + 127).to(U8)[..., 0]
 
 
 def _pages(case, count, g):
@@ -272,7 +277,7 @@ def _values(held, scales, page, place):
     if scales is None:
         return held[page, place].float()
     codes = held.view(U8)[page, place].view(torch.float8_e4m3fn).float()
-    return torch.ldexp(codes, scales[page, place].int()[..., None] - 127)
+    return codes * _power(scales[page, place].int()[..., None] - 127)
 
 
 def _attn(s):
