@@ -8,7 +8,7 @@
 // so a thread keeps the sines of its four (or eight) pairs and walks heads.  An angle is formed in 64 bits: positions go to 2^31, and
 // in 32 bits the angle of position 100 000 is off by 4e-3.  What is left of it after the whole turns, rounded to 32 bits, goes to
 // the sine and cosine instructions, which take turns.
-#include "element.h"
+#include "rope.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -30,15 +30,6 @@ struct RopeParams {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeAhead = 4;    // heads of a thread in flight
-constexpr int kRopeMostHeads = 1 << 16;
-
-// A source beyond the L2s passes them by, and a result beyond the last-level cache passes that by as well.  Measured with the kernel that reads
-// the result: 113 MB 43.9 us, sources past 38.6, results too 43.3; 737 MB 267, 262, 253; 28 MB 19.3, 21.4, 23.5.  A smaller result of
-// whole lines of 128 bytes is written through the L2s as it comes (12 MB 6.0 us, so 5.2; 57 MB 21.4 and 19.4, in place 21.0 and 17.8, with its
-// reader 38.4 and 36.5; 184 MB 65.3 and 60.3; only 111 MB in place lose, 36.7 and 41.8).
-constexpr int64_t kRopeL2 = 32 << 20, kRopeLastLevel = 256 << 20;
-enum RopeSource { kThroughCaches, kPastL2 };
-enum RopeResult { kKept, kWrittenThrough, kPastLastLevel };
 
 // A thread's item of a row: ADJACENT pairs (elements 2j, 2j + 1), eight elements that hold four pairs; HALVES (elements j, j +
 // pairs), the eight elements of eight pairs in either half.  Items behind the pairs are copied.
@@ -51,17 +42,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
     const int turned = p.pairs / NP;                     // items that hold pairs
     const bool turn = item < turned;
     const int64_t e0 = HALVES && !turn ? 2 * p.pairs + (item - turned) * 8 : item * 8, e1 = HALVES && turn ? e0 + p.pairs : e0;
-    auto load = [](const uint16_t* at) {
-        const u32x4* words = reinterpret_cast<const u32x4*>(at);
-        return SOURCE == kPastL2 ? __builtin_nontemporal_load(words) : *words;
-    };
+    auto load = [](const uint16_t* at) { return rope_load<SOURCE>(at); };
     const __amdgpu_buffer_rsrc_t result = raw_buffer(p.out, INT32_MAX);   // (a result that is written through reaches no further)
-    auto store = [&](uint16_t* at, u32x4 value) {
-        u32x4* words = reinterpret_cast<u32x4*>(at);
-        if (RESULT == kWrittenThrough) __builtin_amdgcn_raw_buffer_store_b128(value, result, (int)((at - p.out) * 2), 0, 16);   // sc1
-        else if (RESULT == kPastLastLevel) __builtin_nontemporal_store(value, words);
-        else *words = value;
-    };
+    auto store = [&](uint16_t* at, u32x4 value) { rope_store<RESULT>(result, p.out, at, value); };
     const int last_head = min(p.heads, ((int)blockIdx.y + 1) * p.side * p.per);
     for (int64_t t = (int64_t)blockIdx.x * p.at_once + in_group; t < p.tokens; t += (int64_t)gridDim.x * p.at_once) {
         float c[NP], s[NP];
@@ -70,10 +53,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
 #pragma unroll
             for (int i = 0; i < NP; i++) {
                 const int j = item * NP + i;
-                double turns = (double)(j < p.end0 ? at[0] : j < p.end1 ? at[1] : at[2]) * p.freqs[j] * 0.15915494309189533577;
-                turns -= __builtin_rint(turns);
-                c[i] = __builtin_amdgcn_cosf((float)turns);
-                s[i] = __builtin_amdgcn_sinf((float)turns) * p.sign;
+                rope_turn(j < p.end0 ? at[0] : j < p.end1 ? at[1] : at[2], p.freqs[j], c[i], s[i]);
+                s[i] *= p.sign;
             }
         }
         const uint16_t* from = p.x + t * p.x_token;
@@ -134,14 +115,9 @@ extern "C" int32_t chipmunk_rope(const uint16_t* x, int64_t x_token_stride, int6
     const int64_t pairs = (int64_t)pairs_t + pairs_h + pairs_w;
     if (pairs <= 0 || 2 * pairs > E) return CHIPMUNK_ERR_SHAPE;
     if (E % 8 != 0 || E > 512 || pairs % (halves ? 8 : 4) != 0 || (dtype != CHIPMUNK_DTYPE_BF16 && dtype != CHIPMUNK_DTYPE_FP16)) return CHIPMUNK_ERR_UNSUPPORTED;
-    // rows of heads do not overlap: one of the two strides is a row's length at least, and the other the rows it spans
-    auto overlap = [&](int64_t token, int64_t head) {
-        return !((tokens == 1 || token >= (__int128)(heads - 1) * head + E) && (heads == 1 || head >= E)) &&
-               !((heads == 1 || head >= (__int128)(tokens - 1) * token + E) && (tokens == 1 || token >= E));
-    };
     if (tokens == 1) x_token_stride = out_token_stride = 0;   // of one row alone a stride means nothing
     if (heads == 1) x_head_stride = out_head_stride = 0;
-    if (overlap(x_token_stride, x_head_stride) || overlap(out_token_stride, out_head_stride)) return CHIPMUNK_ERR_SHAPE;
+    if (rope_rows_overlap(x_token_stride, x_head_stride, tokens, heads, E) || rope_rows_overlap(out_token_stride, out_head_stride, tokens, heads, E)) return CHIPMUNK_ERR_SHAPE;
     if (!aligned16(x) || !aligned16(out) || (reinterpret_cast<uintptr_t>(pos) & 3) || (reinterpret_cast<uintptr_t>(freqs) & 7) ||
         (x_token_stride | x_head_stride | out_token_stride | out_head_stride) % 8 != 0)
         return CHIPMUNK_ERR_ALIGN;
