@@ -332,6 +332,79 @@ int32_t chipmunk_attn_packed(const uint16_t* q, int64_t q_token_stride, int64_t 
                              int S, int Tq, int Tk, int Hq, int Hk, int E, int max_q, int max_k, int causal,
                              float softmax_scale, int dtype, void* ws, size_t ws_bytes, void* stream);
 
+/* RMS norm of every head and the rotary positions behind it, of queries and keys in one pass: with r = 1 / sqrt(mean_e x[t,h,e]^2 + eps),
+ *   out[t,h] = turn(x[t,h] r w),   w = q_weight for the first q_heads heads, k_weight for the others,
+ * turn and the layouts as chipmunk_rope has them (no pairs: none, pos and freqs may be NULL); products in fp32, rounded once.
+ * q_weight, k_weight: [E], of the elements' type (NULL where no head has it).  eps in [2^-126, inf).  out may be x (same pointer and
+ * strides) and overlaps nothing else. */
+int32_t chipmunk_norm_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_head_stride, const uint16_t* q_weight, const uint16_t* k_weight, int q_heads,
+                           const int32_t* pos, const double* freqs, uint16_t* out, int64_t out_token_stride, int64_t out_head_stride, int tokens, int heads,
+                           int E, int pairs_t, int pairs_h, int pairs_w, float eps, int halves, int dtype, void* stream);
+
+/* Its gradient.  grad: of out; x: as chipmunk_norm_rope had it.  With g = turn^-1(grad), n = x r, c = mean_e(g_e w_e n_e):
+ *   dx[t,h] = r (g w - n c);   dq_weight[e], dk_weight[e] = sum of g_e n_e over the tokens and the heads that have the weight
+ * (fp32 [E], written; NULL where no head has it; a sum's order depends on the sizes alone).  dx may be grad or x (same pointer and
+ * strides) and overlaps nothing else.  ws: chipmunk_norm_rope_grad_workspace_bytes() (0 on bad arguments), contents undefined
+ * afterwards, not to be shared by calls that may overlap. */
+size_t chipmunk_norm_rope_grad_workspace_bytes(int tokens, int heads, int E);
+int32_t chipmunk_norm_rope_grad(const uint16_t* grad, int64_t grad_token_stride, int64_t grad_head_stride, const uint16_t* x, int64_t x_token_stride,
+                                int64_t x_head_stride, const uint16_t* q_weight, const uint16_t* k_weight, int q_heads, const int32_t* pos,
+                                const double* freqs, uint16_t* dx, int64_t dx_token_stride, int64_t dx_head_stride, float* dq_weight, float* dk_weight,
+                                int tokens, int heads, int E, int pairs_t, int pairs_h, int pairs_w, float eps, int halves, int dtype, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/* ---- Keys and values of many sequences in pages of page_size tokens each.  Row r of the pages is token r % page_size of page
+ * r / page_size.  The elements are of the calls' type, or e4m3 (OCP: 4 exponent bits, 3 of the fraction) under a power of two for
+ * each row of a head: the row stands for code * 2^(scale - 127), rounded to the calls' type.  A power of two costs e4m3 nothing
+ * but range and makes the way back exact. ---- */
+
+#define CHIPMUNK_DTYPE_E4M3  2   /* of pages only */
+
+typedef struct {
+    void* k;                 /* element e of head h of token t of page g at g * page_stride + t * token_stride + h * head_stride + e */
+    void* v;                 /* by the same strides */
+    uint8_t* k_scales;       /* e4m3: [page, token, head] by the scales' strides; else NULL */
+    uint8_t* v_scales;
+    int64_t page_stride, token_stride, head_stride;                     /* elements, of rows that do not overlap; multiples of 16 bytes */
+    int64_t scale_page_stride, scale_token_stride, scale_head_stride;
+    int32_t pages, page_size, heads, E;   /* page_size a power of two from 16 to 65536; pages * page_size < 2^31; E in {64,128}; token strides < 2^24 */
+    int32_t format;                       /* CHIPMUNK_DTYPE_*: that of the calls, or E4M3 */
+} chipmunk_pages;
+
+/* Writes keys and values of new tokens to their rows of the pages.  k, v: [tokens, heads, E], any strides of rows that do not overlap;
+ * rows: int64 [tokens]; a token whose row is negative, or behind the last page, is not written.  No row may be named twice: what it then
+ * holds is undefined (of that row alone).
+ * e4m3: 2^k, k = scale - 127, is the least power at which the row's largest magnitude is 448 at most (k >= -126; a row of zeros: 0);
+ * code = x 2^-k rounded to nearest even.  Infinities and NaN become NaN and do not count for the power; magnitudes above 1.875 * 2^127 (fp16:
+ * 1.875 * 2^15) are taken as that, so that no value comes back infinite. */
+int32_t chipmunk_cache_write(const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride, const uint16_t* v, int64_t v_token_stride,
+                             int64_t v_head_stride, const int64_t* rows, const chipmunk_pages* pages, int tokens, int dtype, void* stream);
+
+/* Rows of the pages back as elements: k, v: [tokens, heads, E], any strides of rows that do not overlap.  Rows may be named more than once;
+ * where one is negative, or behind the last page, k and v are left as they are. */
+int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_t* rows, uint16_t* k, int64_t k_token_stride, int64_t k_head_stride, uint16_t* v,
+                            int64_t v_token_stride, int64_t v_head_stride, int tokens, int dtype, void* stream);
+
+/* Attention of new tokens over S sequences in pages, heads grouped: query head h reads the pages' head h / (Hq / heads).  Sequence s has the queries
+ * cu_q[s] .. cu_q[s+1] - 1 of q (n_q of them) and k_len[s] keys (n_k of them, the new tokens' among them, written before), key j in place j %
+ * page_size of page table[s][j / page_size].  Its query i stands at i + n_k - n_q and sees key j if not `causal`, or if j is not behind it and,
+ * with a window > 0 (causal only), j > i + n_k - n_q - window or j < sinks.
+ *   out[i,h] = softmax_j(softmax_scale * <q[i,h], k[j]>) v[j]     over the keys that are seen; none: zero.
+ * As chipmunk_attn_packed: scores, softmax and sums in fp32, a probability rounded to the element type where it meets v, and no influence of
+ * what is not seen, whatever the pages hold there; of e4m3 pages k and v are the rows that chipmunk_cache_read gives.
+ * q, out: element e of head h of row t at t * token stride + h * head stride + e, token and head stride >= E; out overlaps nothing
+ * else; its rows that belong to no sequence are left as they were.  table: int32 [S][table_pages], row stride table_stride; entries behind a
+ * sequence's last page are not read; a page that the pages do not have reads as zeros.  max_q, max_k: no sequence has more queries, keys;
+ * sequences that do are cut there, which gives wrong results, as do bad entries of cu_q and k_len, without accesses outside the tensors.
+ * They may be far too large.  table_pages * page_size <= 2^30; softmax_scale in (0, 2^127]; token strides < 2^24.
+ * ws: chipmunk_attn_paged_workspace_bytes() (0: ws may be NULL; also 0 on bad arguments) of the same sizes, contents undefined afterwards,
+ * not to be shared by calls that may overlap. */
+size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks);
+int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
+                            int64_t table_stride, int table_pages, uint16_t* out, int64_t out_token_stride, int64_t out_head_stride, const int32_t* cu_q,
+                            const int32_t* k_len, int S, int Tq, int Hq, int max_q, int max_k, int causal, int window, int sinks, float softmax_scale,
+                            int dtype, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -57,6 +57,16 @@ _SIGNATURES = {
     "chipmunk_rope": ([_c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_i64] + [_c_int] * 9 + [_c_ptr], ctypes.c_int32),
     "chipmunk_attn_packed_workspace_bytes": ([_c_int] * 6, _c_size),
     "chipmunk_attn_packed": ([_c_ptr, _c_i64, _c_i64] * 4 + [_c_ptr] * 3 + [_c_int] * 9 + [_c_f32, _c_int, _c_ptr, _c_size, _c_ptr], ctypes.c_int32),
+    "chipmunk_norm_rope": ([_c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_i64] + [_c_int] * 6 + [_c_f32, _c_int, _c_int, _c_ptr],
+                           ctypes.c_int32),
+    "chipmunk_norm_rope_grad_workspace_bytes": ([_c_int] * 3, _c_size),
+    "chipmunk_norm_rope_grad": ([_c_ptr, _c_i64, _c_i64] * 2 + [_c_ptr, _c_ptr, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr] + [_c_int] * 6 +
+                                [_c_f32, _c_int, _c_int, _c_ptr, _c_size, _c_ptr], ctypes.c_int32),
+    "chipmunk_cache_write": ([_c_ptr, _c_i64, _c_i64] * 2 + [_c_ptr, _c_ptr, _c_int, _c_int, _c_ptr], ctypes.c_int32),
+    "chipmunk_cache_read": ([_c_ptr, _c_ptr] + [_c_ptr, _c_i64, _c_i64] * 2 + [_c_int, _c_int, _c_ptr], ctypes.c_int32),
+    "chipmunk_attn_paged_workspace_bytes": ([_c_int] * 8, _c_size),
+    "chipmunk_attn_paged": ([_c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr, _c_i64, _c_int, _c_ptr, _c_i64, _c_i64, _c_ptr, _c_ptr] + [_c_int] * 8 + [_c_f32, _c_int, _c_ptr, _c_size, _c_ptr],
+                            ctypes.c_int32),
     "chipmunk_status_string": ([ctypes.c_int32], ctypes.c_char_p),
 }
 
@@ -91,7 +101,7 @@ def _bind(lib):
         warnings.warn(f"the compiled binding is not used ({e}): calls take some 2 us longer (build() makes it anew)", RuntimeWarning)
         return _Python()
     names = ("voxel_reorder", "topk_cols", "attn_sparse_delta", "attn_dense", "attn_dense_colsum_stale", "mlp_tile_mean_preact",
-             "mlp_sparse_delta", "mlp_dense", "linear", "rope", "attn_packed")
+             "mlp_sparse_delta", "mlp_dense", "linear", "rope", "attn_packed", "norm_rope", "cache_write", "cache_read", "attn_paged")
     _native.bind({"chipmunk_" + n: ctypes.cast(getattr(lib, "chipmunk_" + n), _c_ptr).value for n in names}, _current_device, _raw_stream)
     return _native
 
@@ -487,3 +497,167 @@ def attn_packed(q, k, v, cu_q, cu_k, out, max_q, max_k, causal, softmax_scale, k
     _check(load().chipmunk_attn_packed(pq, strides[0], strides[1], pk, strides[2], strides[3], pv, strides[4], strides[5], po, strides[6], strides[7],
                                        pcq, pck, pkl, S, Tq, Tk, Hq, Hk, E, _int(max_q, "max_q"), _int(max_k, "max_k"), int(bool(causal)), float(softmax_scale), number,
                                        pws, 0 if ws is None else ws.numel(), _stream()), "chipmunk_attn_packed")
+
+
+# ---- normed queries and keys, paged caches, attention over them -----------------------------------------------------------
+
+def _norm_arguments(x, q_weight, k_weight, q_heads, pos, freqs, out, axes):
+    """Checks that norm_rope and its gradient share; the pointers of weights, positions and frequencies, the axes, the element type's number."""
+    dtype, number = _element(x, "x")
+    px, po = _strided(x, dtype, "x", 3), _strided(out, dtype, "out", 3)
+    pq, pk = _strided(q_weight, dtype, "q_weight", 1), _strided(k_weight, dtype, "k_weight", 1)
+    pp, pf = _strided(pos, torch.int32, "pos", 2), _strided(freqs, torch.float64, "freqs", 1)
+    t, h, w = (_int(n, "axes") for n in axes)
+    if out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    if any(weight is not None and weight.shape[0] != x.shape[2] for weight in (q_weight, k_weight)):
+        raise ValueError("q_weight and k_weight must be as long as a head")
+    if pos is not None and (tuple(pos.shape) != (x.shape[0], 3) or not pos.is_contiguous()) or freqs is not None and freqs.shape[0] != t + h + w:
+        raise ValueError("pos must be contiguous [tokens, 3], freqs [pairs of all axes]")
+    return px, po, pq, pk, _int(q_heads, "q_heads"), pp, pf, (t, h, w), number
+
+
+def norm_rope(x, q_weight, k_weight, q_heads, pos, freqs, out, axes, eps=1e-6, halves=False):
+    """RMS norm of every head, then rotary positions as rope has them.  x, out: [tokens, heads, E] bf16 or fp16, any strides of tokens and heads; the
+    first q_heads heads are scaled by q_weight [E], the others by k_weight [E]; axes of no pairs: no rotation (pos and freqs None).  out may be x."""
+    status = _fast.norm_rope(x, q_weight, k_weight, q_heads, pos, freqs, out, axes, eps, halves)
+    if status is not None:
+        return _check(status, "chipmunk_norm_rope")
+    px, po, pq, pk, q_heads, pp, pf, axes, number = _norm_arguments(x, q_weight, k_weight, q_heads, pos, freqs, out, axes)
+    tokens, heads, E = x.shape
+    _check(load().chipmunk_norm_rope(px, x.stride(0), x.stride(1), pq, pk, q_heads, pp, pf, po, out.stride(0), out.stride(1), tokens, heads, E, *axes, float(eps),
+                                     int(bool(halves)), number, _stream()), "chipmunk_norm_rope")
+
+
+def norm_rope_grad_workspace_bytes(tokens, heads, E):
+    return int(load().chipmunk_norm_rope_grad_workspace_bytes(_int(tokens, "tokens"), _int(heads, "heads"), _int(E, "E")))
+
+
+def norm_rope_grad(grad, x, q_weight, k_weight, q_heads, pos, freqs, dx, dq_weight, dk_weight, axes, eps=1e-6, halves=False, ws=None):
+    """The gradient of norm_rope.  grad (of its result), x (as it had it), dx: [tokens, heads, E], any strides of tokens and heads, dx may be grad or x;
+    dq_weight, dk_weight: fp32 [E]; ws: uint8 workspace of norm_rope_grad_workspace_bytes."""
+    px, pd, pq, pk, q_heads, pp, pf, axes, number = _norm_arguments(x, q_weight, k_weight, q_heads, pos, freqs, dx, axes)
+    pg, pws = _strided(grad, x.dtype, "grad", 3), _strided(ws, torch.uint8, "ws", 1, most=2 ** 63 - 1)
+    pdq, pdk = _strided(dq_weight, torch.float32, "dq_weight", 1), _strided(dk_weight, torch.float32, "dk_weight", 1)
+    tokens, heads, E = x.shape
+    if grad.shape != x.shape or any(d is not None and d.shape[0] != E for d in (dq_weight, dk_weight)):
+        raise ValueError("grad must have the shape of x, dq_weight and dk_weight be as long as a head")
+    _check(load().chipmunk_norm_rope_grad(pg, grad.stride(0), grad.stride(1), px, x.stride(0), x.stride(1), pq, pk, q_heads, pp, pf, pd, dx.stride(0), dx.stride(1), pdq, pdk,
+                                          tokens, heads, E, *axes, float(eps), int(bool(halves)), number, pws, 0 if ws is None else ws.numel(), _stream()),
+           "chipmunk_norm_rope_grad")
+
+
+class _PagesStruct(ctypes.Structure):
+    _fields_ = ([(name, _c_ptr) for name in ("k", "v", "k_scales", "v_scales")] +
+                [(name, _c_i64) for name in ("page_stride", "token_stride", "head_stride", "scale_page_stride", "scale_token_stride", "scale_head_stride")] +
+                [(name, ctypes.c_int32) for name in ("pages", "page_size", "heads", "E", "format")])
+
+
+class Pages:
+    """Keys and values of many sequences in pages, checked once.  k, v: [pages, page_size, heads, E] of one shape, type and strides, bf16 or fp16 as
+    the calls' tensors or float8_e4m3fn, then with k_scales, v_scales: uint8 [pages, page_size, heads], exponent + 127 of each row's power of
+    two, of one set of strides too (a page's scales of one head side by side are read fastest).  Holds the tensors."""
+
+    def __init__(self, k, v, k_scales=None, v_scales=None):
+        if not isinstance(k, torch.Tensor) or k.dtype not in _FORMATS:
+            raise TypeError("k: expected a torch tensor of bfloat16, float16 or float8_e4m3fn")
+        codes = k.dtype is torch.float8_e4m3fn
+        if (k_scales is not None or v_scales is not None) != codes or (codes and (k_scales is None or v_scales is None)):
+            raise ValueError("k_scales and v_scales go with float8_e4m3fn, and with nothing else")
+        s = _PagesStruct(_strided(k, k.dtype, "k", 4), _strided(v, k.dtype, "v", 4), _paged_scales(k_scales, "k_scales"), _paged_scales(v_scales, "v_scales"))
+        if v.shape != k.shape or v.stride() != k.stride():
+            raise ValueError("v must have the shape and strides of k")
+        if codes and (tuple(k_scales.shape) != tuple(k.shape[:3]) or v_scales.shape != k_scales.shape or v_scales.stride() != k_scales.stride()):
+            raise ValueError("k_scales and v_scales must be [pages, page_size, heads], of the same strides")
+        s.page_stride, s.token_stride, s.head_stride = k.stride()[:3]
+        if codes:
+            s.scale_page_stride, s.scale_token_stride, s.scale_head_stride = k_scales.stride()
+        s.pages, s.page_size, s.heads, s.E = k.shape
+        s.format = _FORMATS[k.dtype]
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.device, self._struct = k.device.index, s
+        self._address = ctypes.addressof(s)
+        self._plain = (self._address, self.device, s.heads, s.E)   # what the compiled binding reads
+
+    def rows(self):
+        """Tokens that the pages hold."""
+        return self._struct.pages * self._struct.page_size
+
+
+_FORMATS = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
+
+def _paged_scales(t, name):
+    """Pointer of the scales, whose last dimension need not be dense; None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8:
+        raise TypeError(f"{name}: expected a torch tensor of {torch.uint8}")
+    if t.dim() != 3:
+        raise ValueError(f"{name}: must have 3 dimensions")
+    if t.device.type != "cuda" or t.device.index != _device():
+        raise ValueError(f"{name}: must live on the current device")
+    return t.data_ptr()
+
+
+def _pages_of(pages):
+    if not isinstance(pages, Pages):
+        raise TypeError("pages: expected Pages")
+    if pages.device != _device():
+        raise ValueError("pages: must live on the current device")
+    return pages._address
+
+
+def _cache_arguments(k, v, rows, pages):
+    dtype, number = _element(k, "k")
+    pk, pv, pr, pp = _strided(k, dtype, "k", 3), _strided(v, dtype, "v", 3), _strided(rows, torch.int64, "rows", 1), _pages_of(pages)
+    if v.shape != k.shape or rows.shape[0] != k.shape[0] or tuple(k.shape[1:]) != tuple(pages.k.shape[2:]):
+        raise ValueError("k and v must be [tokens, heads, E] with the pages' heads and E, rows [tokens]")
+    return pk, pv, pr, pp, number
+
+
+def cache_write(k, v, rows, pages):
+    """Keys and values of new tokens to their rows of the pages.  k, v: [tokens, heads, E] bf16 or fp16, any strides of tokens and heads; rows: int64 [tokens],
+    page * page_size + place, negative: not written; no row twice."""
+    status = _fast.cache_write(k, v, rows, getattr(pages, "_plain", None))
+    if status is not None:
+        return _check(status, "chipmunk_cache_write")
+    pk, pv, pr, pp, number = _cache_arguments(k, v, rows, pages)
+    _check(load().chipmunk_cache_write(pk, k.stride(0), k.stride(1), pv, v.stride(0), v.stride(1), pr, pp, k.shape[0], number, _stream()), "chipmunk_cache_write")
+
+
+def cache_read(pages, rows, k, v):
+    """Rows of the pages back as elements: k, v: [tokens, heads, E] bf16 or fp16 (written; where a row is negative, left alone); rows: int64 [tokens]."""
+    status = _fast.cache_read(getattr(pages, "_plain", None), rows, k, v)
+    if status is not None:
+        return _check(status, "chipmunk_cache_read")
+    pk, pv, pr, pp, number = _cache_arguments(k, v, rows, pages)
+    _check(load().chipmunk_cache_read(pp, pr, pk, k.stride(0), k.stride(1), pv, v.stride(0), v.stride(1), k.shape[0], number, _stream()), "chipmunk_cache_read")
+
+
+def attn_paged_workspace_bytes(S, Hq, Hk, E, max_q, max_k, window=0, sinks=0):
+    sizes = dict(S=S, Hq=Hq, Hk=Hk, E=E, max_q=max_q, max_k=max_k, window=window, sinks=sinks)
+    return int(load().chipmunk_attn_paged_workspace_bytes(*(_int(n, name) for name, n in sizes.items())))
+
+
+def attn_paged(q, pages, table, cu_q, k_len, out, max_q, max_k, causal, softmax_scale, window=0, sinks=0, ws=None):
+    """Attention of new tokens over sequences in pages.  q, out: [Tq, Hq, E] bf16 or fp16, any strides of rows and heads; pages: Pages; table: int32
+    [S, most pages], rows dense, the pages of each sequence in order; cu_q: int32 [S + 1], where the sequences' queries start; k_len: int32 [S],
+    tokens that each sequence holds, the new ones among them; max_q, max_k: no sequence has more queries, keys; window: keys that a query
+    sees, itself the last (0: all); sinks: first tokens that stay visible; ws: uint8 workspace of attn_paged_workspace_bytes (none needed where that is 0)."""
+    status = _fast.attn_paged(q, getattr(pages, "_plain", None), table, cu_q, k_len, out, max_q, max_k, causal, softmax_scale, window, sinks, ws)
+    if status is not None:
+        return _check(status, "chipmunk_attn_paged")
+    dtype, number = _element(q, "q")
+    i32 = torch.int32
+    pq, po, pp = _strided(q, dtype, "q", 3), _strided(out, dtype, "out", 3), _pages_of(pages)
+    pt, pc, pl = _strided(table, i32, "table", 2), _strided(cu_q, i32, "cu_q", 1), _strided(k_len, i32, "k_len", 1)
+    pws = _strided(ws, torch.uint8, "ws", 1, most=2 ** 63 - 1)
+    (Tq, Hq, E), S = q.shape, k_len.shape[0]
+    if out.shape != q.shape or pages.k.shape[3] != E:
+        raise ValueError("out must have the shape of q, and the pages the same E")
+    if cu_q.shape[0] != S + 1 or table.shape[0] != S:
+        raise ValueError("cu_q must be [sequences + 1], table [sequences, pages], k_len [sequences]")
+    _check(load().chipmunk_attn_paged(pq, q.stride(0), q.stride(1), pp, pt, table.stride(0), table.shape[1], po, out.stride(0), out.stride(1), pc, pl, S, Tq, Hq,
+                                      _int(max_q, "max_q"), _int(max_k, "max_k"), int(bool(causal)), _int(window, "window"), _int(sinks, "sinks"), float(softmax_scale),
+                                      number, pws, 0 if ws is None else ws.numel(), _stream()), "chipmunk_attn_paged")

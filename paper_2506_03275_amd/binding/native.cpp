@@ -22,8 +22,10 @@ Entry entries[] = {{"chipmunk_voxel_reorder", nullptr},       {"chipmunk_topk_co
                    {"chipmunk_attn_dense_colsum_stale", nullptr}, {"chipmunk_mlp_tile_mean_preact", nullptr},
                    {"chipmunk_mlp_sparse_delta", nullptr},    {"chipmunk_mlp_dense", nullptr},
                    {"chipmunk_linear", nullptr},              {"chipmunk_rope", nullptr},
-                   {"chipmunk_attn_packed", nullptr}};
-enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense, kLinear, kRope, kAttnPacked };
+                   {"chipmunk_attn_packed", nullptr},         {"chipmunk_norm_rope", nullptr},
+                   {"chipmunk_cache_write", nullptr},         {"chipmunk_cache_read", nullptr},
+                   {"chipmunk_attn_paged", nullptr}};
+enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense, kLinear, kRope, kAttnPacked, kNormRope, kCacheWrite, kCacheRead, kAttnPaged };
 PyObject* current_device = nullptr;   // torch's functions that name the current device and, for a device, its current stream
 PyObject* raw_stream = nullptr;
 
@@ -372,6 +374,110 @@ PyObject* attn_packed(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// Three sizes in a list or a tuple
+struct Axes {
+    int t = 0, h = 0, w = 0;
+    Axes(Args& a, int i) {
+        if (!a.ok || (!PyList_CheckExact(a.v[i]) && !PyTuple_CheckExact(a.v[i])) || PySequence_Fast_GET_SIZE(a.v[i]) != 3) {
+            a.ok = false;
+            return;
+        }
+        Args axes{PySequence_Fast_ITEMS(a.v[i]), true};
+        t = axes.integer(0), h = axes.integer(1), w = axes.integer(2);
+        a.ok = axes.ok;
+    }
+    int64_t pairs() const { return (int64_t)t + h + w; }
+};
+
+// x, q_weight, k_weight, q_heads, pos, freqs, out, axes, eps, halves
+PyObject* norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kNormRope, args, n, 10, [](Args& a, auto run) {
+        Strided s(a, 0);
+        const at::Tensor *x = s.elements(0, 3), *wq = s.optional(1, 1, s.element), *wk = s.optional(2, 1, s.element), *pos = s.optional(4, 2, at::kInt),
+                         *freqs = s.optional(5, 1, at::kDouble), *out = s.elements(6, 3);
+        const int q_heads = a.integer(3);
+        const Axes axes(a, 7);
+        const float eps = a.real(8);
+        const bool halves = s.truth(9);
+        if (!a.ok || out->sizes() != x->sizes() || (wq && wq->size(0) != x->size(2)) || (wk && wk->size(0) != x->size(2)) ||
+            (pos && (pos->size(0) != x->size(0) || pos->size(1) != 3 || !pos->is_contiguous())) || (freqs && freqs->size(0) != axes.pairs())) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_norm_rope){}, elements_of(x), x->stride(0), x->stride(1), elements_of(wq), elements_of(wk), q_heads, pos ? (const int32_t*)pos->data_ptr() : nullptr,
+            freqs ? (const double*)freqs->data_ptr() : nullptr, const_cast<uint16_t*>(elements_of(out)), out->stride(0), out->stride(1), (int)x->size(0), (int)x->size(1),
+            (int)x->size(2), axes.t, axes.h, axes.w, eps, (int)halves, s.number(), stream);
+    });
+}
+
+// What a Pages object says of itself: the address of its struct, its device, heads and E
+struct PagesArg {
+    const chipmunk_pages* at = nullptr;
+    int heads = 0, E = 0;
+    PagesArg(Strided& s, int i) {
+        Args& a = s.a;
+        if (!a.ok || !PyTuple_CheckExact(a.v[i]) || PyTuple_GET_SIZE(a.v[i]) != 4) {
+            a.ok = false;
+            return;
+        }
+        at = static_cast<const chipmunk_pages*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(a.v[i], 0)));
+        Args rest{PySequence_Fast_ITEMS(a.v[i]), true};
+        const int device = rest.integer(1);
+        heads = rest.integer(2), E = rest.integer(3);
+        if (PyErr_Occurred() || !rest.ok || !at || device != s.device) a.ok = false;
+    }
+};
+
+// k, v, rows, pages (writing) or pages, rows, k, v (reading)
+template <class Run>
+void cache_call(Args& a, int k_at, int v_at, int rows_at, int pages_at, Run&& run) {
+    Strided s(a, k_at);
+    const at::Tensor *k = s.elements(k_at, 3), *v = s.elements(v_at, 3), *rows = s.tensor(rows_at, 1, at::kLong);
+    const PagesArg pages(s, pages_at);
+    if (!a.ok || v->sizes() != k->sizes() || rows->size(0) != k->size(0) || k->size(1) != pages.heads || k->size(2) != pages.E) {
+        a.ok = false;
+        return;
+    }
+    run(s, k, v, (const int64_t*)rows->data_ptr(), pages.at, a.stream());
+}
+PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kCacheWrite, args, n, 4, [](Args& a, auto run) {
+        cache_call(a, 0, 1, 2, 3, [&](Strided& s, const at::Tensor* k, const at::Tensor* v, const int64_t* rows, const chipmunk_pages* pages, void* stream) {
+            run(decltype(&chipmunk_cache_write){}, elements_of(k), k->stride(0), k->stride(1), elements_of(v), v->stride(0), v->stride(1), rows, pages, (int)k->size(0), s.number(), stream);
+        });
+    });
+}
+PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kCacheRead, args, n, 4, [](Args& a, auto run) {
+        cache_call(a, 2, 3, 1, 0, [&](Strided& s, const at::Tensor* k, const at::Tensor* v, const int64_t* rows, const chipmunk_pages* pages, void* stream) {
+            run(decltype(&chipmunk_cache_read){}, pages, rows, const_cast<uint16_t*>(elements_of(k)), k->stride(0), k->stride(1), const_cast<uint16_t*>(elements_of(v)), v->stride(0),
+                v->stride(1), (int)k->size(0), s.number(), stream);
+        });
+    });
+}
+
+// q, pages, table, cu_q, k_len, out, max_q, max_k, causal, softmax_scale, window, sinks, ws
+PyObject* attn_paged(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kAttnPaged, args, n, 13, [](Args& a, auto run) {
+        Strided s(a, 0);
+        const at::Tensor *q = s.elements(0, 3), *table = s.tensor(2, 2, at::kInt), *cu_q = s.tensor(3, 1, at::kInt), *k_len = s.tensor(4, 1, at::kInt), *out = s.elements(5, 3),
+                         *ws = s.optional(12, 1, at::kByte);
+        const PagesArg pages(s, 1);
+        const int max_q = a.integer(6), max_k = a.integer(7), window = a.integer(10), sinks = a.integer(11);
+        const bool causal = s.truth(8);
+        const float scale = a.real(9);
+        if (!a.ok || out->sizes() != q->sizes() || q->size(2) != pages.E || cu_q->size(0) != k_len->size(0) + 1 || table->size(0) != k_len->size(0)) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_attn_paged){}, elements_of(q), q->stride(0), q->stride(1), pages.at, (const int32_t*)table->data_ptr(), table->stride(0), (int)table->size(1),
+            const_cast<uint16_t*>(elements_of(out)), out->stride(0), out->stride(1), (const int32_t*)cu_q->data_ptr(), (const int32_t*)k_len->data_ptr(), (int)k_len->size(0),
+            (int)q->size(0), (int)q->size(1), max_q, max_k, (int)causal, window, sinks, scale, s.number(), ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->numel() : (size_t)0, stream);
+    });
+}
+
 // bind(addresses: dict of names, current_device, raw_stream)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 3 || !PyDict_Check(args[0])) {
@@ -393,7 +499,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(voxel_reorder), FAST(topk_cols), FAST(attn_sparse_delta), FAST(attn_dense),
                          FAST(attn_dense_colsum_stale), FAST(mlp_tile_mean_preact), FAST(mlp_sparse_delta), FAST(mlp_dense),
-                         FAST(linear), FAST(rope), FAST(attn_packed),
+                         FAST(linear), FAST(rope), FAST(attn_packed), FAST(norm_rope), FAST(cache_write), FAST(cache_read), FAST(attn_paged),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,700 @@
+// Attention of new tokens over sequences in pages (chipmunk_pages): one token of a sequence, a few or a chunk of them, causal or not, every key or
+// a sliding window and the sequence's first keys; pages of 16 bits, or e4m3 whose rows are brought to the element type on their way to LDS, so that
+// a call over codes gives bit by bit what it gives over the elements that they stand for.
+//
+// The kernels are those of attention over packed sequences (attn_packed.hip, attn_tiles.h) with other keys: a workgroup walks a row of "numbered" keys,
+// those that some of its rows may see (the first ones, then, behind a gap, the window's), and what it has at hand of the table are the rows of the pages at which
+// groups of 16 numbered keys begin, in LDS.  A group lies in one page, so a transfer's base is in scalar registers and its lanes' offsets never change.
+#include "attn_tiles.h"
+#include "pages.h"
+
+#include <type_traits>
+
+namespace chipmunk {
+
+struct PagedParams : AttnParams {
+    chipmunk_pages pages;
+    const int32_t* table;
+    const int32_t* k_len;
+    int64_t table_row;       // stride of the table's rows
+    int most_keys;           // of a sequence: by the limit and by the table
+    int window, sinks;       // window 0: every key
+    int shift;               // log2 of the page's tokens
+    int block_rows;          // few queries: rows of a workgroup
+};
+
+constexpr int kGroup = 16;                    // keys that lie in one page, side by side
+constexpr int kTableKeys = 4096;              // keys of a part of the table in LDS
+constexpr int kTableGroups = kTableKeys / kGroup;
+
+__device__ __forceinline__ int keys_held(const PagedParams& p, int s) { return min(max(p.k_len[s], 0), p.most_keys); }
+
+// The first key that query i does not see, and the first of its window.
+__device__ __forceinline__ int limit_of(const PagedParams& p, int i, int keys, int past) { return p.causal ? min(keys, i + 1 + past) : keys; }
+__device__ __forceinline__ int low_of(const PagedParams& p, int i, int past) { return p.window ? max(max(i + 1 + past, 0) - p.window, 0) : 0; }
+
+// The keys that rows of queries first .. last walk, numbered from 0: key n for n < edge, key n + jump from there on.
+struct Walk {
+    int sinks, end, edge, jump, count;        // end: the first key that none of the rows sees; count: of numbered keys
+    __device__ __forceinline__ int key(int n) const { return n < edge ? n : n + jump; }
+};
+template <int STEP>
+__device__ __forceinline__ Walk walk_of(const PagedParams& p, int first, int last, int keys, int past) {
+    Walk k;
+    k.sinks = p.window ? min(p.sinks, keys) : 0;
+    k.end = max(limit_of(p, last, keys, past), 0);
+    const int low = low_of(p, first, past) / STEP * STEP;
+    k.edge = (int)(((uint32_t)k.sinks + STEP - 1) / STEP * STEP);
+    k.jump = low - k.edge;
+    if (k.jump <= 0) k.edge = k.jump = 0;
+    k.count = max(k.end - k.jump, 0);
+    return k;
+}
+
+// Numbered keys n .. n + 16 groups' rows of the pages (-1: none), by the threads of a workgroup.
+__device__ __forceinline__ void fill_table(const PagedParams& p, const Walk& walk, int s, int first, int groups, int32_t* to) {
+    for (int i = threadIdx.x; i < groups; i += 256) {
+        const int64_t n = (int64_t)first + i * kGroup;
+        int row = -1;
+        if (n < walk.count) {
+            const int key = walk.key((int)n);
+            const int page = p.table[s * p.table_row + (key >> p.shift)];
+            if (page >= 0 && page < p.pages.pages) row = (page << p.shift) + (key & (p.pages.page_size - 1));
+        }
+        to[i] = row;
+    }
+}
+
+// Of a group: its first row's place in the pages (elements; scales), and how many of its keys there are.
+struct Group {
+    int64_t at, scale_at;
+    int rows;
+};
+__device__ __forceinline__ Group group_of(const PagedParams& p, int row, int head, int key, int end) {
+    const int page = row >> p.shift, place = row & (p.pages.page_size - 1);
+    return Group{page * p.pages.page_stride + place * p.pages.token_stride + head * p.pages.head_stride,
+                 page * p.pages.scale_page_stride + place * p.pages.scale_token_stride + head * p.pages.scale_head_stride, row < 0 ? 0 : min(max(end - key, 0), kGroup)};
+}
+// A buffer over a group's rows: what lies behind the last key reads as zero.
+__device__ __forceinline__ i32x4 group_words(const void* base, const Group& g, int64_t token, int E) {
+    return raw_buffer_words(static_cast<const uint16_t*>(base) + (g.rows > 0 ? g.at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * token + E) * 2u : 0u);
+}
+
+// Rows of codes in registers, on their way to a tile: NL loads of 16 codes a lane, ROWS_A_LOAD rows each.
+template <int E, int NL>
+struct Codes {
+    static constexpr int LANES = E / 16, ROWS_A_LOAD = 64 / LANES;
+    u32x4 code[NL];
+    uint32_t scale[NL];
+    // load i: rows first .. first + ROWS_A_LOAD of a group
+    __device__ __forceinline__ void request(int i, const PagedParams& p, const void* base, const uint8_t* scales, const Group& g, int first, int lane) {
+        const int row = first + lane / LANES;
+        const int64_t token = p.pages.token_stride, scale_token = p.pages.scale_token_stride;
+        const auto rows = raw_buffer(static_cast<const uint8_t*>(base) + (g.rows > 0 ? g.at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * token + E) : 0u);
+        const auto bytes = raw_buffer(scales + (g.rows > 0 ? g.scale_at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * scale_token + 1) : 0u);
+        code[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, row * (int)token + lane % LANES * 16, 0, 0));
+        scale[i] = __builtin_amdgcn_raw_buffer_load_b8(bytes, row * (int)scale_token, 0, 0);
+    }
+    // to row `row` of the tile at LDS address `tile`, as elements
+    template <class T>
+    __device__ __forceinline__ void put(int i, uint32_t tile, int row, int lane) const {
+        const float power = __uint_as_float(scale[i] << 23);
+        const int swizzle = tile_swizzle<E>(row);
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+            const u32x2 a = elements_of_codes<T>(code[i][2 * c], power), b = elements_of_codes<T>(code[i][2 * c + 1], power);
+            const uint32_t to = tile + (uint32_t)(row * E * 2 + (((lane % LANES * 2 + c) ^ swizzle) * 16));
+            *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)to) = u32x4{a[0], a[1], b[0], b[1]};
+        }
+    }
+};
+
+// The keys of a tile that a query does not see: from its limit on, and between the first ones and its window.
+template <int NQB>
+__device__ __forceinline__ void hide_far_keys(f32x4 (&S)[2][NQB], int first, const int (&low)[NQB], int sinks) {
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++) {
+        const int from = low[qb] - first, shown = sinks - first;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                S[u][qb][r] = u * 16 + r < from && u * 16 + r >= shown ? -INFINITY : S[u][qb][r];
+                asm volatile("" : "+v"(S[u][qb][r]));
+            }
+    }
+}
+
+// Adds the infinite and NaN values of 32 keys from key `first` on to the queries that see them (tile_values leaves them out where something
+// is hidden).  Rare: the table is read from memory.
+template <class T, int E, int NQB, bool CODES>
+__device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, const PagedParams& p, int s, int head, int first, int end, int sinks, const int (&limit)[NQB],
+                                                   const int (&low)[NQB], int g) {
+#pragma unroll 1
+    for (int key = first; key < min(first + kTile, end); key++) {
+        const int page = p.table[s * p.table_row + (key >> p.shift)];
+        if (page < 0 || page >= p.pages.pages) continue;
+        const Group at = group_of(p, (page << p.shift) + (key & (p.pages.page_size - 1)), head, key, end);
+        float power = 0.f;
+        if (CODES) power = __uint_as_float((uint32_t)p.pages.v_scales[at.scale_at] << 23);
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) {
+            u32x2 words;
+            if constexpr (CODES) words = elements_of_codes<T>(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.pages.v) + at.at + eb * 16 + 4 * g), power);
+            else words = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p.pages.v) + at.at + eb * 16 + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                float value = r % 2 ? T::high(words[r / 2]) : T::low(words[r / 2]);
+                const bool special = not_finite<T>(words[r / 2]) & (r % 2 ? 0x80000000u : 0x8000u);
+                asm volatile("" : "+v"(value));           // nothing is known of it, not even that it is none of the two
+#pragma unroll
+                for (int qb = 0; qb < NQB; qb++)
+                    if (special && key < limit[qb] && (key >= low[qb] || key < sinks)) st.O[eb][qb][r] += value;
+            }
+        }
+    }
+}
+
+// Few queries over many keys, as attn_packed_few_kernel: a workgroup owns one key head of one sequence and walks part_keys of its numbered keys for
+// block_rows rows of the head; its waves take the tiles of 32 keys in turn and meet at the end.
+template <class T, int E, int NQB, bool CODES>
+__global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(PagedParams p) {
+    typedef typename T::x8 x8;
+    constexpr int ROWB = E * 2, CH = ROWB / 16, RPI = 64 / CH, NI = kTile / RPI;   // NI: transfers of a tile
+    constexpr int TILE = kTile * ROWB, NL = kTile * E / 1024;                      // NL: loads of a tile's codes
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    __shared__ int32_t groups[kTableGroups];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, l16 = lane & 15;
+    int id = (int)(blockIdx.x / p.Hk);
+    const int head = (int)blockIdx.x % p.Hk, part = id % p.parts;
+    id /= p.parts;
+    const int row0 = (p.tiles - 1 - id % p.tiles) * 16 * NQB, s = id / p.tiles;
+    const Rows qs = queries_of(p, s);
+    const int rows = min(16 * NQB, qs.count * p.G - row0);
+    if (rows <= 0) return;
+    const int keys = keys_held(p, s), past = keys - qs.count;
+    const int i0 = row0 / p.G, i1 = (row0 + rows - 1) / p.G;
+    const Walk walk = walk_of<kTile>(p, i0, i1, keys, past);
+    const int seen_by_all = limit_of(p, i0, keys, past), low_of_all = low_of(p, i1, past);
+    const int64_t start64 = (int64_t)part * p.part_keys;
+    if (start64 >= walk.count && part > 0) return;        // (without any key the first part writes zeros)
+    const int start = (int)start64, whole_end = (int)std::min<int64_t>(walk.count, start64 + p.part_keys);
+
+    RowState<T, E, NQB> st;
+    int limit[NQB], low[NQB];                             // the first key that the lane's row does not see; the first of its window
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++) {
+        st.negm[qb] = st.L[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) st.O[eb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int row = row0 + min(qb * 16 + l16, rows - 1), i = row / p.G;   // (rows that are not there: the last one's)
+        limit[qb] = limit_of(p, i, keys, past);
+        low[qb] = low_of(p, i, past);
+        const uint16_t* from = p.q + (int64_t)(qs.first + i) * p.q_token + (head * p.G + row % p.G) * p.q_head + 8 * g;
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) {
+            u32x4 val = u32x4{0, 0, 0, 0};
+            if (qb * 16 + l16 < rows) val = *reinterpret_cast<const u32x4*>(from + 32 * es);
+            st.Q[es][qb] = __builtin_bit_cast(x8, val);
+        }
+    }
+    const float slack = kSlack / p.sl2;
+
+    const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
+    const int vrow = 4 * g + (l16 >> 2);
+    const int voff = vrow * ROWB + ((((l16 & 3) >> 1) ^ tile_swizzle<E>(vrow)) * 16) + 8 * (l16 & 1);
+    const uint32_t smem_at = (uint32_t)(uintptr_t)CHIPMUNK_LDS_PTR(smem) + w * 2 * TILE;
+    uint32_t kaddr[E / 32], vaddr[E / 16];
+#pragma unroll
+    for (int es = 0; es < E / 32; es++) kaddr[es] = smem_at + (uint32_t)(koff ^ (64 * es));
+#pragma unroll
+    for (int eb = 0; eb < E / 16; eb++) vaddr[eb] = smem_at + (uint32_t)(voff ^ (32 * eb));
+    const uint32_t lds0 = lds_address(smem) + (uint32_t)(w * 2 * TILE);
+    const int64_t token = p.pages.token_stride;
+    constexpr int NIG = NI / 2;                           // transfers of a group: a lane's offsets into it stay the same
+    uint32_t from[NIG];
+#pragma unroll
+    for (int i = 0; i < NIG; i++) {
+        const int row = i * RPI + lane / CH;
+        from[i] = (uint32_t)row * (uint32_t)(token * 2) + (uint32_t)(((lane % CH) ^ tile_swizzle<E>(row)) * 16);
+    }
+    int table_first = start, end = whole_end;             // the numbered keys that the table has
+    auto group = [&](int n, int u) {                      // group u of the tile from numbered key n on
+        const bool there = n < end;                       // (behind the part's end nothing is requested)
+        const int at = there ? (n - table_first) / kGroup + u : 0;
+        const int row = __builtin_amdgcn_readfirstlane(groups[at]);
+        return group_of(p, there ? row : -1, head, walk.key(n) + u * kGroup, walk.end);
+    };
+    Codes<E, NL> k_codes, v_codes;
+    auto request = [&](const void* base, const uint8_t* scales, Codes<E, NL>& codes, int n, uint32_t to) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const Group at = group(n, u);
+            if constexpr (CODES) {
+                constexpr int ROWS = Codes<E, NL>::ROWS_A_LOAD;
+#pragma unroll
+                for (int i = u * NL / 2; i < (u + 1) * NL / 2; i++) codes.request(i, p, base, scales, at, i * ROWS % kGroup, lane);
+            } else {
+                const i32x4 buf = group_words(base, at, token, E);
+#pragma unroll
+                for (int i = 0; i < NIG; i++) load_buffer_to_lds_16B(buf, from[i], to + (u * NIG + i) * 1024);
+            }
+        }
+    };
+    auto put = [&](const Codes<E, NL>& codes, uint32_t tile) {
+        constexpr int ROWS = Codes<E, NL>::ROWS_A_LOAD;
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < NL; i++) codes.template put<T>(i, tile, i * ROWS + lane / Codes<E, NL>::LANES, lane);
+        asm volatile("" ::: "memory");                    // (a wave's LDS accesses are done in order)
+    };
+    auto request_k = [&](int n) { request(p.pages.k, p.pages.k_scales, k_codes, n, lds0); };
+    auto request_v = [&](int n) { request(p.pages.v, p.pages.v_scales, v_codes, n, lds0 + TILE); };
+    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
+    uint32_t found = 0;
+    auto is_plain = [&](int key) { return key + kTile <= seen_by_all && (key >= low_of_all || key + kTile <= walk.sinks); };
+    auto tile = [&](auto hidden_c, int n, int key) {
+        constexpr bool HIDDEN = decltype(hidden_c)::value;
+        f32x4 S[2][NQB];
+        if constexpr (CODES) {
+            put(k_codes, lds0);
+            request_k(n + TURN);
+        } else {
+            wait_vmem_at_most<NI>();                      // K has landed
+            asm volatile("" ::: "memory");
+        }
+        tile_scores<T, E, NQB>(S, st, kaddr, 0, [](int) {});
+        if constexpr (!CODES) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and has been read
+            request_k(n + TURN);
+        }
+        if (HIDDEN) {
+            hide_keys<NQB>(S, key + 4 * g, limit);
+            if (p.window) hide_far_keys<NQB>(S, key + 4 * g, low, walk.sinks);
+        }
+        raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+        if constexpr (CODES) {
+            put(v_codes, lds0 + TILE);
+            request_v(n + TURN);
+        } else {
+            wait_vmem_at_most<NI>();                      // V
+            asm volatile("" ::: "memory");
+        }
+        tile_values<T, E, NQB, HIDDEN>(st, S, vaddr, TILE, p.sl2, found);
+        if constexpr (!CODES) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            request_v(n + TURN);
+        }
+    };
+#pragma unroll 1
+    for (; table_first < whole_end; table_first += kTableKeys) {   // (once, where a part is no longer than the table)
+        if (table_first > start) __syncthreads();         // every wave is done with the table
+        end = min(whole_end, table_first + kTableKeys);
+        fill_table(p, walk, s, table_first, (end - table_first + kGroup - 1) / kGroup, groups);
+        wait_all_memory();                                // the table and, the first time, the queries
+        __syncthreads();
+        int n = table_first + w * kTile;
+        if (n < end) {
+            request_k(n);
+            request_v(n);
+        }
+#pragma unroll 1
+        for (; n < end; n += TURN) {
+            const int key = walk.key(n);
+            if (is_plain(key)) tile(std::false_type{}, n, key);
+            else tile(std::true_type{}, n, key);
+        }
+        wait_all_memory();
+        if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
+#pragma unroll 1
+            for (n = table_first + w * kTile; n < end; n += TURN) {
+                const int key = walk.key(n);
+                if (!is_plain(key)) add_special_values<T, E, NQB, CODES>(st, p, s, head, key, walk.end, walk.sinks, limit, low, g);
+            }
+        found = 0;
+    }
+    lds_accesses_then_barrier();                          // every wave is done with its tiles
+    const bool alone = walk.count <= p.part_keys;
+    join_waves<T, E, NQB>(st, smem, w, lane, p.sl2, [&](int qb, const f32x4 (&o)[E / 64], float top, float total) {
+        const int row = row0 + qb * 16 + l16;
+        if (row < row0 + rows) store_joined<T, E>(p, s, head, part, qs.first, row, alone, limit[qb] > 0, w, g, o, top, total);
+    });
+}
+
+// Rows, as attn_packed_rows_kernel: a workgroup of four waves owns 64 NQB consecutive queries of one sequence and head and walks its numbered keys in steps of
+// two tiles of 32.  Elements go from the pages to LDS by asynchronous loads, double buffered by step; codes are in registers a step before, and go to LDS
+// as elements while the step before theirs is computed.
+template <class T, int E, int NQB, bool CODES>
+__global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) {
+    typedef typename T::x8 x8;
+    constexpr int NWAVES = 4, ROWS = 16 * NQB * NWAVES;
+    constexpr int ROWB = E * 2;                           // bytes per K/V row of a tile
+    constexpr int CH = ROWB / 16, RPI = 64 / CH;          // 16-byte chunks per row; rows covered by one wave-wide load
+    constexpr int NI = kTile / (RPI * NWAVES);            // such loads per wave, tile and matrix
+    constexpr int TILE = kTile * ROWB, STAGE = 2 * TILE;  // K tile then V tile
+    constexpr int NL = kStepKeys * E / 4096;              // loads of a step's codes per wave and matrix
+    constexpr int NG = CODES ? NL : kStepTiles * NI;      // groups of a step that a wave fills rows of
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    __shared__ int32_t groups[2 * kTableGroups];          // of two parts of the keys by turns
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, l16 = lane & 15;
+
+    int tile, head, s, part;
+    tile_and_head(p, blockIdx.x, &tile, &head);
+    if (tile >= p.tiles || !find_tile<ROWS>(p, tile, lane, &s, &part)) return;
+    s = __builtin_amdgcn_readfirstlane(s);
+    part = __builtin_amdgcn_readfirstlane(part);
+    const Rows qs = queries_of(p, s);
+    const int row0 = part * ROWS, rows = min(ROWS, qs.count - row0);
+    if (rows <= 0) return;
+    const int keys = keys_held(p, s), past = keys - qs.count;
+    const Walk walk = walk_of<kStepKeys>(p, row0, row0 + rows - 1, keys, past);
+    const uint16_t* qh = p.q + head * p.q_head + (int64_t)(qs.first + row0) * p.q_token;
+    uint16_t* oh = p.out + head * p.out_head + (int64_t)(qs.first + row0) * p.out_token;
+    const int kv_head = head / p.G;
+
+    RowState<T, E, NQB> st;
+    int limit[NQB], low[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++) {
+        st.negm[qb] = st.L[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) st.O[eb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int row = (w * NQB + qb) * 16 + l16, i = row0 + min(row, rows - 1);   // (rows that are not there: the last one's)
+        limit[qb] = limit_of(p, i, keys, past);
+        low[qb] = low_of(p, i, past);
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) {
+            u32x4 val = u32x4{0, 0, 0, 0};
+            if (row < rows) val = *reinterpret_cast<const u32x4*>(qh + row * p.q_token + 32 * es + 8 * g);
+            st.Q[es][qb] = __builtin_bit_cast(x8, val);
+        }
+    }
+    // what all of a wave's rows see, and what any of them sees
+    const int wave_row = w * NQB * 16, wave_rows = min(rows - wave_row, NQB * 16);
+    const int first_row = row0 + wave_row, last_row = first_row + max(wave_rows, 1) - 1;
+    const int seen = wave_rows <= 0 ? 0 : limit_of(p, last_row, keys, past), seen_by_all = wave_rows <= 0 ? 0 : limit_of(p, first_row, keys, past);
+    const int low_of_any = low_of(p, first_row, past), low_of_all = low_of(p, last_row, past);
+    const float slack = kSlack / p.sl2;
+
+    const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
+    const int vrow = 4 * g + (l16 >> 2);
+    const int voff = vrow * ROWB + ((((l16 & 3) >> 1) ^ tile_swizzle<E>(vrow)) * 16) + 8 * (l16 & 1);
+    const uint32_t smem_at = (uint32_t)(uintptr_t)CHIPMUNK_LDS_PTR(smem);
+    uint32_t kaddr[E / 32], vaddr[E / 16];                // opaque, so that what is added stays in the reads' offset field
+#pragma unroll
+    for (int es = 0; es < E / 32; es++) {
+        kaddr[es] = smem_at + (uint32_t)(koff ^ (64 * es));
+        asm volatile("" : "+v"(kaddr[es]));
+    }
+#pragma unroll
+    for (int eb = 0; eb < E / 16; eb++) {
+        vaddr[eb] = smem_at + (uint32_t)(voff ^ (32 * eb));
+        asm volatile("" : "+v"(vaddr[eb]));
+    }
+    const uint32_t lds0 = lds_address(smem);
+    const int64_t token = p.pages.token_stride;
+
+    // Elements: load (n, i) of a wave fills rows (i * NWAVES + w) * RPI .. of tile n, which are in group 2 n + i (E = 128) or 2 n + w / 2 of the step.
+    // Codes: load i fills rows of group 2 i + w / 2 (E = 128), or of group w.
+    auto group_at = [&](int n) { return E == 128 ? (CODES ? 2 * n + (w >> 1) : n) : (CODES ? w : 2 * n + (w >> 1)); };
+    constexpr int ROWS_A_LOAD = CODES ? Codes<E, NL>::ROWS_A_LOAD : RPI;
+    const int in_group = w * ROWS_A_LOAD % kGroup;        // of the load's first row
+    const int row_of_lane = in_group + lane / CH;
+    const uint32_t from = (uint32_t)row_of_lane * (uint32_t)(token * 2) + (uint32_t)(((lane % CH) ^ tile_swizzle<E>(row_of_lane)) * 16);   // (elements)
+    Group at[NG];                                         // of the step that is requested next
+    auto next_step = [&](int n) {
+#pragma unroll
+        for (int i = 0; i < NG; i++) {
+            const int u = group_at(i);
+            const int row = __builtin_amdgcn_readfirstlane(groups[(n / kGroup + u) % (2 * kTableGroups)]);
+            at[i] = group_of(p, n < walk.count ? row : -1, kv_head, walk.key(n) + u * kGroup, walk.end);
+        }
+    };
+    Codes<E, CODES ? NL : 1> k_codes, v_codes;
+    auto request = [&](int half, int j) {
+        const int n = j / (2 * NI), i = (j / 2) % NI;
+        const uint32_t to = lds0 + (uint32_t)((half * kStepTiles + n) * STAGE + (i * NWAVES + w) * 1024);
+        const Group& from_group = at[CODES ? 0 : n * NI + i];
+        if (j & 1) load_buffer_to_lds_16B(group_words(p.pages.v, from_group, token, E), from, to + TILE);
+        else load_buffer_to_lds_16B(group_words(p.pages.k, from_group, token, E), from, to);
+    };
+    static_assert(kStepTiles * NI * 2 == E / 16, "one transfer per group of score products");
+    auto request_codes = [&]() {
+        if constexpr (CODES) {
+#pragma unroll
+            for (int i = 0; i < NL; i++) {
+                k_codes.request(i, p, p.pages.k, p.pages.k_scales, at[i], in_group, lane);
+                v_codes.request(i, p, p.pages.v, p.pages.v_scales, at[i], in_group, lane);
+            }
+        }
+    };
+    auto put_codes = [&](int half) {
+        if constexpr (CODES) {
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < NL; i++) {
+                const int row = group_at(i) * kGroup + in_group + lane / Codes<E, NL>::LANES;   // of the step
+                const uint32_t to = lds0 + (uint32_t)((half * kStepTiles + group_at(i) / 2) * STAGE);
+                k_codes.template put<T>(i, to, row % kTile, lane);
+                v_codes.template put<T>(i, to + TILE, row % kTile, lane);
+            }
+            asm volatile("" ::: "memory");
+        }
+    };
+
+    if (walk.count > 0) {
+        fill_table(p, walk, s, 0, walk.count > kTableKeys ? 2 * kTableGroups : kTableGroups, groups);
+        wait_all_memory();                                // no wait for the queries inside the loop
+        __syncthreads();
+        next_step(0);
+        if constexpr (CODES) {
+            request_codes();
+            put_codes(0);
+            next_step(kStepKeys);
+            request_codes();
+        } else {
+#pragma unroll
+            for (int j = 0; j < E / 16; j++) request(0, j);
+        }
+    }
+    // Begins the step from numbered key n on, whose tiles are in half `half`.
+    auto arrived = [&](int n, int half) {
+        if constexpr (CODES) lds_accesses_then_barrier();  // the codes stay under way
+        else wait_all_memory(), __syncthreads();          // this step's tiles have landed for every wave; the other half is free
+        if (n % kTableKeys == 0 && n > 0 && n + kTableKeys < walk.count)
+            fill_table(p, walk, s, n + kTableKeys, kTableGroups, groups + (n / kTableKeys + 1) % 2 * kTableGroups);   // (many barriers before its first use)
+        if constexpr (CODES) {
+            put_codes(half ^ 1);
+            next_step(n + 2 * kStepKeys);
+            request_codes();
+        } else {
+            next_step(n + kStepKeys);
+        }
+    };
+    // The steps whose keys all of the wave's rows see, two at a time, whose LDS offsets are constants; and one by one those with hidden keys, and
+    // what is left over.  Waves may stand in different ones: each step of each is one barrier.
+    uint32_t found = 0;
+    auto step = [&](auto half_c, int n) {
+        constexpr int half = decltype(half_c)::value;
+        arrived(n, half);
+#pragma unroll
+        for (int t = 0; t < kStepTiles; t++) {
+            const int tile_off = (half * kStepTiles + t) * STAGE;
+            f32x4 S[2][NQB];
+            if (t == 0 && !CODES) tile_scores<T, E, NQB>(S, st, kaddr, tile_off, [&](int j) { request(half ^ 1, j); });
+            else tile_scores<T, E, NQB>(S, st, kaddr, tile_off, [](int) {});
+            raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+            tile_values<T, E, NQB, false>(st, S, vaddr, tile_off + TILE, p.sl2, found);
+        }
+    };
+    int moved = 0;                                        // where the addresses stand
+    auto hidden_step = [&](int n, int half) {
+        arrived(n, half);
+        if constexpr (!CODES) {
+#pragma unroll
+            for (int j = 0; j < E / 16; j++) request(half ^ 1, j);
+        }
+        const int key = walk.key(n);
+        if (key >= seen || (key + kStepKeys <= low_of_any && key >= walk.sinks)) return;   // nothing to see for this wave
+        const int bytes = (half - moved) * kStepTiles * STAGE;
+        moved = half;
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
+#pragma unroll
+        for (int t = 0; t < kStepTiles; t++) {
+            f32x4 S[2][NQB];
+            tile_scores<T, E, NQB>(S, st, kaddr, t * STAGE, [](int) {});
+            hide_keys<NQB>(S, key + t * kTile + 4 * g, limit);
+            if (p.window) hide_far_keys<NQB>(S, key + t * kTile + 4 * g, low, walk.sinks);
+            raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+            tile_values<T, E, NQB, true>(st, S, vaddr, t * STAGE + TILE, p.sl2, found);
+        }
+    };
+    auto is_plain = [&](int n) {
+        const int key = walk.key(n);
+        return n < walk.count && key + kStepKeys <= seen_by_all && (key >= low_of_all || key + kStepKeys <= walk.sinks);
+    };
+    auto goes_in_pairs = [&](int n, int half) { return half == 0 && is_plain(n) && is_plain(n + kStepKeys); };
+    int half = 0;
+#pragma unroll 1
+    for (int n = 0; n < walk.count;) {
+        if (goes_in_pairs(n, half)) {
+            if (moved) {
+                moved = 0;
+#pragma unroll
+                for (int es = 0; es < E / 32; es++) kaddr[es] -= kStepTiles * STAGE;
+#pragma unroll
+                for (int eb = 0; eb < E / 16; eb++) vaddr[eb] -= kStepTiles * STAGE;
+            }
+#pragma unroll 1
+            do {
+                step(std::integral_constant<int, 0>{}, n);
+                step(std::integral_constant<int, 1>{}, n + kStepKeys);
+                n += 2 * kStepKeys;
+            } while (goes_in_pairs(n, 0));
+        } else {
+            hidden_step(n, half);
+            n += kStepKeys;
+            half ^= 1;
+        }
+    }
+    wait_all_memory();                                    // the transfers behind the last step
+
+    // Infinite and NaN values among the steps that went one by one go to the queries that see them.
+    if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
+        half = 0;
+#pragma unroll 1
+        for (int n = 0; n < walk.count;) {
+            if (goes_in_pairs(n, half)) {
+                n += 2 * kStepKeys;
+                continue;
+            }
+            const int key = walk.key(n);
+            if (key < seen && !(key + kStepKeys <= low_of_any && key >= walk.sinks))
+#pragma unroll 1
+                for (int t = 0; t < kStepTiles; t++)
+                    add_special_values<T, E, NQB, CODES>(st, p, s, kv_head, key + t * kTile, walk.end, walk.sinks, limit, low, g);
+            n += kStepKeys;
+            half ^= 1;
+        }
+    }
+    store_rows<T, E, NQB>(st, limit, oh, p.out_token, w * NQB * 16, rows, g, l16);
+}
+
+// Joins the parts of the rows that have more than one: a wave per row.
+template <class T, int E>
+__global__ __launch_bounds__(256) void attn_paged_join_kernel(PagedParams p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= (int64_t)p.S * p.Hk * p.few_rows) return;
+    const int row = (int)(id % p.few_rows), head = (int)(id / p.few_rows % p.Hk), s = (int)(id / p.few_rows / p.Hk);
+    const Rows qs = queries_of(p, s);
+    if (row >= qs.count * p.G) return;
+    const int keys = keys_held(p, s), past = keys - qs.count;
+    const int row0 = row / p.block_rows * p.block_rows, rows = min(p.block_rows, qs.count * p.G - row0);   // the workgroup's that had it
+    const Walk walk = walk_of<kTile>(p, row0 / p.G, (row0 + rows - 1) / p.G, keys, past);
+    if (walk.count <= p.part_keys) return;
+    join_parts<T, E>(p, s, head, row, qs.first, min((walk.count - 1) / p.part_keys + 1, p.parts), limit_of(p, row / p.G, keys, past) > 0, lane);
+}
+
+// The numbered keys that a workgroup has at most: its rows' queries, at most max_q of them, see as many more than a window, in steps of `step`.
+static int most_numbered(int max_q, int max_k, int window, int sinks, int step) {
+    if (window == 0) return max_k;
+    const int64_t most = (int64_t)window + max_q + sinks + 2 * step;
+    return (int)std::min<int64_t>(most, max_k);
+}
+
+template <class T, int E, int NQB, bool CODES>
+static int32_t launch_paged_rows(PagedParams p, hipStream_t stream) {
+    constexpr int ROWS = 64 * NQB, LDS = 2 * kStepTiles * 2 * kTile * E * 2;
+    const auto kernel = attn_paged_rows_kernel<T, E, NQB, CODES>;
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
+    const PackedGrid grid = rows_grid(ROWS, p.S, p.Tq, p.Hq, p.Hk, p.max_q);
+    p.tiles = (int)grid.tiles;
+    kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
+    return launch_status();
+}
+
+template <class T, int E, int NQB, bool CODES>
+static int32_t launch_paged_few(PagedParams p, hipStream_t stream) {
+    constexpr int TOGETHER = NQB < 2 ? NQB : 2;
+    constexpr int LDS = std::max(4 * 2 * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
+    const auto kernel = attn_paged_few_kernel<T, E, NQB, CODES>;
+    const PackedGrid grid = few_grid(16 * NQB, p.S, p.Hk, p.few_rows, p.parts);
+    if (grid.workgroups >= kMostWorkgroups) return CHIPMUNK_ERR_SHAPE;
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
+    p.tiles = (int)grid.tiles;
+    p.block_rows = 16 * NQB;
+    kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
+    if (p.parts > 1) attn_paged_join_kernel<T, E><<<(uint32_t)(((int64_t)p.S * p.Hk * p.few_rows + 3) / 4), 256, 0, stream>>>(p);
+    return launch_status();
+}
+
+template <class T, int E, bool CODES>
+static int32_t launch_paged(PagedParams p, const FewPlan& few, int most_keys, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (few.rows > 0) {
+        if (few_bytes(few, p.S, p.Hk, E) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
+        p.few_rows = few.rows;
+        p.part_keys = few.part_keys;
+        p.parts = few.parts;
+        p.partial = static_cast<float*>(ws);
+        return few.rows <= 16   ? launch_paged_few<T, E, 1, CODES>(p, stream)
+               : few.rows <= 32 ? launch_paged_few<T, E, 2, CODES>(p, stream)
+                                : launch_paged_few<T, E, 4, CODES>(p, stream);
+    }
+    const PackedForm form = packed_form(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, most_keys, p.causal);
+    if (packed_price(form, p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, most_keys, p.causal) == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;   // no form's launch covers it
+    if (form <= kKeys32) {
+        p.few_rows = p.max_q * p.G;
+        p.part_keys = INT32_MAX;
+        p.parts = 1;
+    }
+    switch (form) {
+        case kKeys16: return launch_paged_few<T, E, 1, CODES>(p, stream);
+        case kKeys32: return launch_paged_few<T, E, 2, CODES>(p, stream);
+        case kRows64: return launch_paged_rows<T, E, 1, CODES>(p, stream);
+        case kRows128: return launch_paged_rows<T, E, 2, CODES>(p, stream);
+        default: return launch_paged_rows<T, E, 3, CODES>(p, stream);
+    }
+}
+
+}  // namespace chipmunk
+
+using namespace chipmunk;
+
+// The keys that a plan divides: those that are numbered, in whole tiles.
+static int planned_keys(int max_q, int max_k, int window, int sinks) { return most_numbered(max_q, max_k, window, sinks, kStepKeys); }
+
+extern "C" size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks) {
+    if (S <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (E != 64 && E != 128) || max_q <= 0 || max_k <= 0 || window < 0 || sinks < 0) return 0;
+    return few_bytes(few_plan(S, Hq, Hk, max_q, planned_keys(max_q, max_k, window, sinks)), S, Hk, E);
+}
+
+extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
+                                       int64_t table_stride, int table_pages, uint16_t* out, int64_t out_token_stride, int64_t out_head_stride, const int32_t* cu_q,
+                                       const int32_t* k_len, int S, int Tq, int Hq, int max_q, int max_k, int causal, int window, int sinks, float softmax_scale,
+                                       int dtype, void* ws, size_t ws_bytes, void* stream) {
+    if (!q || !pages || !table || !out || !cu_q || !k_len) return CHIPMUNK_ERR_NULL;
+    chipmunk_pages held = *pages;
+    const int32_t status = check_pages(held, dtype);
+    if (status != CHIPMUNK_OK) return status;
+    const int Hk = held.heads, E = held.E;
+    if (S <= 0 || Tq <= 0 || Hq <= 0 || Hq % Hk != 0 || max_q <= 0 || max_k <= 0 || table_pages <= 0 || window < 0 || sinks < 0 || (window > 0 && !causal)) return CHIPMUNK_ERR_SHAPE;
+    if ((int64_t)table_pages * held.page_size > (1 << 30)) return CHIPMUNK_ERR_SHAPE;
+    const float sl2 = softmax_scale * 1.4426950408889634f;
+    if (!is_positive_finite_scalar(softmax_scale) || !is_finite_scalar(sl2)) return CHIPMUNK_ERR_SHAPE;
+    constexpr int64_t kMostStride = 1 << 24;
+    if (Tq == 1) q_token_stride = out_token_stride = E;   // of one row alone a stride means nothing
+    if (S == 1) table_stride = table_pages;
+    for (int64_t token : {q_token_stride, out_token_stride})
+        if (token < E || token >= kMostStride) return CHIPMUNK_ERR_SHAPE;
+    if (table_stride < table_pages || (Hq > 1 && (q_head_stride < E || out_head_stride < E))) return CHIPMUNK_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(ws) ||
+        ((reinterpret_cast<uintptr_t>(cu_q) | reinterpret_cast<uintptr_t>(k_len) | reinterpret_cast<uintptr_t>(table)) & 3) ||
+        (q_token_stride | out_token_stride) % 8 != 0 || (Hq > 1 && (q_head_stride | out_head_stride) % 8 != 0))
+        return CHIPMUNK_ERR_ALIGN;
+    const int most_keys = std::min(max_k, table_pages * held.page_size);
+    const int given = planned_keys(max_q, max_k, window, sinks);   // as the workspace was asked for
+    if (window >= most_keys) window = 0;                  // (which every query sees whole)
+    PagedParams p{{q, out, cu_q, q_token_stride, q_head_stride, out_token_stride, out_head_stride, S, Tq, Hq, Hk, Hq / Hk, std::min(max_q, Tq), most_keys, causal != 0, 0, 0, 0, 0,
+                   nullptr, sl2},
+                  held, table, k_len, table_stride, most_keys, window, window ? sinks : 0, __builtin_ctz((uint32_t)held.page_size), 0};
+    const int planned = planned_keys(max_q, most_keys, window, sinks);
+    const FewPlan few = few_plan_within(S, Hq, Hk, max_q, given, planned);
+    const auto st = static_cast<hipStream_t>(stream);
+    auto go = [&](auto type, auto width) {
+        typedef decltype(type) T;
+        constexpr int W = decltype(width)::value;
+        return held.format == CHIPMUNK_DTYPE_E4M3 ? launch_paged<T, W, true>(p, few, planned, ws, ws_bytes, st) : launch_paged<T, W, false>(p, few, planned, ws, ws_bytes, st);
+    };
+    typedef std::integral_constant<int, 64> Narrow;
+    typedef std::integral_constant<int, 128> Wide;
+    if (dtype == CHIPMUNK_DTYPE_BF16) return E == 128 ? go(Bf16{}, Wide{}) : go(Bf16{}, Narrow{});
+    return E == 128 ? go(Fp16{}, Wide{}) : go(Fp16{}, Narrow{});
+}
