@@ -3,8 +3,9 @@
 // a call over codes gives bit by bit what it gives over the elements that they stand for.
 //
 // The kernels are those of attention over packed sequences (attn_packed.hip, attn_tiles.h) with other keys: a workgroup walks a row of "numbered" keys,
-// those that some of its rows may see (the first ones, then, behind a gap, the window's), and what it has at hand of the table are the rows of the pages at which
-// groups of 16 numbered keys begin, in LDS.  A group lies in one page, so a transfer's base is in scalar registers and its lanes' offsets never change.
+// those that some of its rows may see, those first that all of them may (an online softmax has no order).  Where groups of 16 numbered keys
+// begin is worked out from the table for 4096 of them at a time, and lies in LDS: a group is in one page, so a transfer's base is in scalar
+// registers and its lanes' offsets never change.
 #include "attn_tiles.h"
 #include "pages.h"
 
@@ -33,51 +34,65 @@ __device__ __forceinline__ int keys_held(const PagedParams& p, int s) { return m
 __device__ __forceinline__ int limit_of(const PagedParams& p, int i, int keys, int past) { return p.causal ? min(keys, i + 1 + past) : keys; }
 __device__ __forceinline__ int low_of(const PagedParams& p, int i, int past) { return p.window ? max(max(i + 1 + past, 0) - p.window, 0) : 0; }
 
-// The keys that rows of queries first .. last walk, numbered from 0: key n for n < edge, key n + jump from there on.
+// The keys that the rows of queries first .. last walk, numbered from 0 in whole steps: from the first that is in every row's window (`high`) to the
+// last; then the sequence's first ones, up to `sinks`; then from the first that is in any row's window (`low`) to `high`.
 struct Walk {
-    int sinks, end, edge, jump, count;        // end: the first key that none of the rows sees; count: of numbered keys
-    __device__ __forceinline__ int key(int n) const { return n < edge ? n : n + jump; }
+    int sinks, end;                           // end: the first key that none of the rows sees
+    int high, low, upto, edge, count;         // numbers below upto, below edge, of all
+    __device__ __forceinline__ int key(int n) const { return n < upto ? high + n : n < edge ? n - upto : n - edge + low; }
 };
 template <int STEP>
 __device__ __forceinline__ Walk walk_of(const PagedParams& p, int first, int last, int keys, int past) {
+    auto whole = [](int n) { return (n + STEP - 1) / STEP * STEP; };
     Walk k;
     k.sinks = p.window ? min(p.sinks, keys) : 0;
     k.end = max(limit_of(p, last, keys, past), 0);
-    const int low = low_of(p, first, past) / STEP * STEP;
-    k.edge = (int)(((uint32_t)k.sinks + STEP - 1) / STEP * STEP);
-    k.jump = low - k.edge;
-    if (k.jump <= 0) k.edge = k.jump = 0;
-    k.count = max(k.end - k.jump, 0);
+    k.high = min(whole(low_of(p, last, past)), whole(k.end));
+    k.low = low_of(p, first, past) / STEP * STEP;
+    int shown = whole(k.sinks);
+    if (shown >= k.low) k.low = shown = 0;    // no gap behind the first ones
+    k.upto = whole(k.end) - k.high;
+    k.edge = k.upto + shown;
+    k.count = k.edge + k.high - k.low;
     return k;
 }
 
-// Numbered keys n .. n + 16 groups' rows of the pages (-1: none), by the threads of a workgroup.
-__device__ __forceinline__ void fill_table(const PagedParams& p, const Walk& walk, int s, int first, int groups, int32_t* to) {
-    for (int i = threadIdx.x; i < groups; i += 256) {
-        const int64_t n = (int64_t)first + i * kGroup;
-        int row = -1;
-        if (n < walk.count) {
-            const int key = walk.key((int)n);
-            const int page = p.table[s * p.table_row + (key >> p.shift)];
-            if (page >= 0 && page < p.pages.pages) row = (page << p.shift) + (key & (p.pages.page_size - 1));
-        }
-        to[i] = row;
-    }
+// Where a group of keys begins: bytes from the pages' first, bytes of its rows up to the last key (0: none), its keys; and its scales.
+struct Place {
+    u32x4 rows;
+    u32x2 scales;
+};
+template <int E, bool CODES>
+__device__ __forceinline__ Place place_of_group(const PagedParams& p, const Walk& walk, int s, int head, int n) {
+    Place to{u32x4{0, 0, 0, 0}, u32x2{0, 0}};
+    const int key = walk.key(n), rows = min(walk.end - key, kGroup);
+    if (n >= walk.count || rows <= 0) return to;
+    const int page = p.table[s * p.table_row + (key >> p.shift)], place = key & (p.pages.page_size - 1);
+    if (page < 0 || page >= p.pages.pages) return to;
+    constexpr int WIDTH = CODES ? 1 : 2;
+    const uint64_t at = (page * p.pages.page_stride + place * p.pages.token_stride + head * p.pages.head_stride) * WIDTH;
+    const uint64_t scales = page * p.pages.scale_page_stride + place * p.pages.scale_token_stride + head * p.pages.scale_head_stride;
+    to.rows = u32x4{(uint32_t)at, (uint32_t)(at >> 32), (uint32_t)((rows - 1) * (int)p.pages.token_stride + E) * WIDTH, (uint32_t)rows};
+    if (CODES) to.scales = u32x2{(uint32_t)scales, (uint32_t)(scales >> 32)};
+    return to;
 }
-
-// Of a group: its first row's place in the pages (elements; scales), and how many of its keys there are.
+// The same in scalar registers; buffers over the rows: what lies behind them reads as zero.
 struct Group {
-    int64_t at, scale_at;
+    uint64_t at, scales;
+    uint32_t bytes;
     int rows;
 };
-__device__ __forceinline__ Group group_of(const PagedParams& p, int row, int head, int key, int end) {
-    const int page = row >> p.shift, place = row & (p.pages.page_size - 1);
-    return Group{page * p.pages.page_stride + place * p.pages.token_stride + head * p.pages.head_stride,
-                 page * p.pages.scale_page_stride + place * p.pages.scale_token_stride + head * p.pages.scale_head_stride, row < 0 ? 0 : min(max(end - key, 0), kGroup)};
-}
-// A buffer over a group's rows: what lies behind the last key reads as zero.
-__device__ __forceinline__ i32x4 group_words(const void* base, const Group& g, int64_t token, int E) {
-    return raw_buffer_words(static_cast<const uint16_t*>(base) + (g.rows > 0 ? g.at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * token + E) * 2u : 0u);
+template <bool CODES>
+__device__ __forceinline__ Group group_of(const u32x4* rows, const u32x2* scales, int i, bool there) {
+    auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    const u32x4 r = rows[i];
+    Group g{(uint64_t)scalar(r[1]) << 32 | scalar(r[0]), 0, there ? scalar(r[2]) : 0u, 0};
+    if (CODES) {
+        const u32x2 c = scales[i];
+        g.scales = (uint64_t)scalar(c[1]) << 32 | scalar(c[0]);
+        g.rows = there ? (int)scalar(r[3]) : 0;
+    }
+    return g;
 }
 
 // Rows of codes in registers, on their way to a tile: NL loads of 16 codes a lane, ROWS_A_LOAD rows each.
@@ -89,11 +104,11 @@ struct Codes {
     // load i: rows first .. first + ROWS_A_LOAD of a group
     __device__ __forceinline__ void request(int i, const PagedParams& p, const void* base, const uint8_t* scales, const Group& g, int first, int lane) {
         const int row = first + lane / LANES;
-        const int64_t token = p.pages.token_stride, scale_token = p.pages.scale_token_stride;
-        const auto rows = raw_buffer(static_cast<const uint8_t*>(base) + (g.rows > 0 ? g.at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * token + E) : 0u);
-        const auto bytes = raw_buffer(scales + (g.rows > 0 ? g.scale_at : 0), g.rows > 0 ? (uint32_t)((g.rows - 1) * scale_token + 1) : 0u);
-        code[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, row * (int)token + lane % LANES * 16, 0, 0));
-        scale[i] = __builtin_amdgcn_raw_buffer_load_b8(bytes, row * (int)scale_token, 0, 0);
+        const int token = (int)p.pages.token_stride, scale_token = (int)p.pages.scale_token_stride;
+        const auto rows = raw_buffer(static_cast<const uint8_t*>(base) + g.at, g.bytes);
+        const auto bytes = raw_buffer(scales + g.scales, g.rows > 0 ? (uint32_t)((g.rows - 1) * scale_token + 1) : 0u);
+        code[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, row * token + lane % LANES * 16, 0, 0));
+        scale[i] = __builtin_amdgcn_raw_buffer_load_b8(bytes, row * scale_token, 0, 0);
     }
     // to row `row` of the tile at LDS address `tile`, as elements
     template <class T>
@@ -134,14 +149,15 @@ __device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, cons
     for (int key = first; key < min(first + kTile, end); key++) {
         const int page = p.table[s * p.table_row + (key >> p.shift)];
         if (page < 0 || page >= p.pages.pages) continue;
-        const Group at = group_of(p, (page << p.shift) + (key & (p.pages.page_size - 1)), head, key, end);
+        const int place = key & (p.pages.page_size - 1);
+        const int64_t at = page * p.pages.page_stride + place * p.pages.token_stride + head * p.pages.head_stride + 4 * g;
         float power = 0.f;
-        if (CODES) power = __uint_as_float((uint32_t)p.pages.v_scales[at.scale_at] << 23);
+        if (CODES) power = __uint_as_float((uint32_t)p.pages.v_scales[page * p.pages.scale_page_stride + place * p.pages.scale_token_stride + head * p.pages.scale_head_stride] << 23);
 #pragma unroll
         for (int eb = 0; eb < E / 16; eb++) {
             u32x2 words;
-            if constexpr (CODES) words = elements_of_codes<T>(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.pages.v) + at.at + eb * 16 + 4 * g), power);
-            else words = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p.pages.v) + at.at + eb * 16 + 4 * g);
+            if constexpr (CODES) words = elements_of_codes<T>(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.pages.v) + at + eb * 16), power);
+            else words = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p.pages.v) + at + eb * 16);
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 float value = r % 2 ? T::high(words[r / 2]) : T::low(words[r / 2]);
@@ -163,7 +179,8 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
     constexpr int ROWB = E * 2, CH = ROWB / 16, RPI = 64 / CH, NI = kTile / RPI;   // NI: transfers of a tile
     constexpr int TILE = kTile * ROWB, NL = kTile * E / 1024;                      // NL: loads of a tile's codes
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    __shared__ int32_t groups[kTableGroups];
+    __shared__ u32x4 places[4][kWave];                    // of each wave's next 32 tiles' groups
+    __shared__ u32x2 scale_places[CODES ? 4 : 1][kWave];
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, l16 = lane & 15;
@@ -177,10 +194,9 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
     const int keys = keys_held(p, s), past = keys - qs.count;
     const int i0 = row0 / p.G, i1 = (row0 + rows - 1) / p.G;
     const Walk walk = walk_of<kTile>(p, i0, i1, keys, past);
-    const int seen_by_all = limit_of(p, i0, keys, past), low_of_all = low_of(p, i1, past);
     const int64_t start64 = (int64_t)part * p.part_keys;
     if (start64 >= walk.count && part > 0) return;        // (without any key the first part writes zeros)
-    const int start = (int)start64, whole_end = (int)std::min<int64_t>(walk.count, start64 + p.part_keys);
+    const int start = (int)start64, end = (int)std::min<int64_t>(walk.count, start64 + p.part_keys);
 
     RowState<T, E, NQB> st;
     int limit[NQB], low[NQB];                             // the first key that the lane's row does not see; the first of its window
@@ -220,12 +236,15 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
         const int row = i * RPI + lane / CH;
         from[i] = (uint32_t)row * (uint32_t)(token * 2) + (uint32_t)(((lane % CH) ^ tile_swizzle<E>(row)) * 16);
     }
-    int table_first = start, end = whole_end;             // the numbered keys that the table has
-    auto group = [&](int n, int u) {                      // group u of the tile from numbered key n on
-        const bool there = n < end;                       // (behind the part's end nothing is requested)
-        const int at = there ? (n - table_first) / kGroup + u : 0;
-        const int row = __builtin_amdgcn_readfirstlane(groups[at]);
-        return group_of(p, there ? row : -1, head, walk.key(n) + u * kGroup, walk.end);
+    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
+    const int first = start + w * kTile;
+    auto fill_table = [&](int n) {                        // the wave's tiles from numbered key n on
+        const Place at = place_of_group<E, CODES>(p, walk, s, head, n + (lane >> 1) * TURN + (lane & 1) * kGroup);
+        places[w][lane] = at.rows;
+        if (CODES) scale_places[CODES ? w : 0][lane] = at.scales;
+    };
+    auto group = [&](int n, int u) {                      // group u of the tile from numbered key n on; nothing behind the part's end
+        return group_of<CODES>(places[w], scale_places[CODES ? w : 0], ((uint32_t)(n - first) / TURN % (kWave / 2)) * 2 + u, n < end);
     };
     Codes<E, NL> k_codes, v_codes;
     auto request = [&](const void* base, const uint8_t* scales, Codes<E, NL>& codes, int n, uint32_t to) {
@@ -237,7 +256,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
 #pragma unroll
                 for (int i = u * NL / 2; i < (u + 1) * NL / 2; i++) codes.request(i, p, base, scales, at, i * ROWS % kGroup, lane);
             } else {
-                const i32x4 buf = group_words(base, at, token, E);
+                const i32x4 buf = raw_buffer_words(static_cast<const uint8_t*>(base) + at.at, at.bytes);
 #pragma unroll
                 for (int i = 0; i < NIG; i++) load_buffer_to_lds_16B(buf, from[i], to + (u * NIG + i) * 1024);
             }
@@ -250,12 +269,14 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
         for (int i = 0; i < NL; i++) codes.template put<T>(i, tile, i * ROWS + lane / Codes<E, NL>::LANES, lane);
         asm volatile("" ::: "memory");                    // (a wave's LDS accesses are done in order)
     };
-    auto request_k = [&](int n) { request(p.pages.k, p.pages.k_scales, k_codes, n, lds0); };
+    auto request_k = [&](int n) {
+        if ((uint32_t)(n - first) % (kWave / 2 * TURN) == 0 && n < end) fill_table(n);
+        request(p.pages.k, p.pages.k_scales, k_codes, n, lds0);
+    };
     auto request_v = [&](int n) { request(p.pages.v, p.pages.v_scales, v_codes, n, lds0 + TILE); };
-    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
     uint32_t found = 0;
-    auto is_plain = [&](int key) { return key + kTile <= seen_by_all && (key >= low_of_all || key + kTile <= walk.sinks); };
-    auto tile = [&](auto hidden_c, int n, int key) {
+    int n = first;
+    auto tile = [&](auto hidden_c) {
         constexpr bool HIDDEN = decltype(hidden_c)::value;
         f32x4 S[2][NQB];
         if constexpr (CODES) {
@@ -271,6 +292,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
             request_k(n + TURN);
         }
         if (HIDDEN) {
+            const int key = walk.key(n);
             hide_keys<NQB>(S, key + 4 * g, limit);
             if (p.window) hide_far_keys<NQB>(S, key + 4 * g, low, walk.sinks);
         }
@@ -288,33 +310,20 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
             request_v(n + TURN);
         }
     };
-#pragma unroll 1
-    for (; table_first < whole_end; table_first += kTableKeys) {   // (once, where a part is no longer than the table)
-        if (table_first > start) __syncthreads();         // every wave is done with the table
-        end = min(whole_end, table_first + kTableKeys);
-        fill_table(p, walk, s, table_first, (end - table_first + kGroup - 1) / kGroup, groups);
-        wait_all_memory();                                // the table and, the first time, the queries
-        __syncthreads();
-        int n = table_first + w * kTile;
-        if (n < end) {
-            request_k(n);
-            request_v(n);
-        }
-#pragma unroll 1
-        for (; n < end; n += TURN) {
-            const int key = walk.key(n);
-            if (is_plain(key)) tile(std::false_type{}, n, key);
-            else tile(std::true_type{}, n, key);
-        }
-        wait_all_memory();
-        if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
-#pragma unroll 1
-            for (n = table_first + w * kTile; n < end; n += TURN) {
-                const int key = walk.key(n);
-                if (!is_plain(key)) add_special_values<T, E, NQB, CODES>(st, p, s, head, key, walk.end, walk.sinks, limit, low, g);
-            }
-        found = 0;
+    wait_all_memory();                                    // the queries
+    if (n < end) {
+        request_k(n);
+        request_v(n);
     }
+    const int plain_end = min(min(end, walk.upto), limit_of(p, i0, keys, past) - walk.high);
+#pragma unroll 1
+    for (; n + kTile <= plain_end; n += TURN) tile(std::false_type{});
+    const int first_hidden = n;
+#pragma unroll 1
+    for (; n < end; n += TURN) tile(std::true_type{});
+    wait_all_memory();
+    if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
+        for (int at = first_hidden; at < end; at += TURN) add_special_values<T, E, NQB, CODES>(st, p, s, head, walk.key(at), walk.end, walk.sinks, limit, low, g);
     lds_accesses_then_barrier();                          // every wave is done with its tiles
     const bool alone = walk.count <= p.part_keys;
     join_waves<T, E, NQB>(st, smem, w, lane, p.sl2, [&](int qb, const f32x4 (&o)[E / 64], float top, float total) {
@@ -337,7 +346,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     constexpr int NL = kStepKeys * E / 4096;              // loads of a step's codes per wave and matrix
     constexpr int NG = CODES ? NL : kStepTiles * NI;      // groups of a step that a wave fills rows of
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    __shared__ int32_t groups[2 * kTableGroups];          // of two parts of the keys by turns
+    __shared__ u32x4 places[2 * kTableGroups];            // of two parts of the keys by turns
+    __shared__ u32x2 scale_places[CODES ? 2 * kTableGroups : 1];
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, l16 = lane & 15;
@@ -376,8 +386,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     // what all of a wave's rows see, and what any of them sees
     const int wave_row = w * NQB * 16, wave_rows = min(rows - wave_row, NQB * 16);
     const int first_row = row0 + wave_row, last_row = first_row + max(wave_rows, 1) - 1;
-    const int seen = wave_rows <= 0 ? 0 : limit_of(p, last_row, keys, past), seen_by_all = wave_rows <= 0 ? 0 : limit_of(p, first_row, keys, past);
-    const int low_of_any = low_of(p, first_row, past), low_of_all = low_of(p, last_row, past);
+    const int seen = wave_rows <= 0 ? 0 : limit_of(p, last_row, keys, past), low_of_any = low_of(p, first_row, past);
+    const int plain_end = wave_rows <= 0 ? 0 : min(walk.upto, limit_of(p, first_row, keys, past) - walk.high);
     const float slack = kSlack / p.sl2;
 
     const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
@@ -408,19 +418,22 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     Group at[NG];                                         // of the step that is requested next
     auto next_step = [&](int n) {
 #pragma unroll
-        for (int i = 0; i < NG; i++) {
-            const int u = group_at(i);
-            const int row = __builtin_amdgcn_readfirstlane(groups[(n / kGroup + u) % (2 * kTableGroups)]);
-            at[i] = group_of(p, n < walk.count ? row : -1, kv_head, walk.key(n) + u * kGroup, walk.end);
-        }
+        for (int i = 0; i < NG; i++) at[i] = group_of<CODES>(places, scale_places, ((uint32_t)n / kGroup + group_at(i)) % (2 * kTableGroups), n < walk.count);
     };
+    auto fill_table = [&](int n) {                        // the part of the keys from n on
+        const int i = (uint32_t)n / kGroup % (2 * kTableGroups) + tid;
+        const Place to = place_of_group<E, CODES>(p, walk, s, kv_head, n + tid * kGroup);
+        places[i] = to.rows;
+        if (CODES) scale_places[CODES ? i : 0] = to.scales;
+    };
+    static_assert(kTableGroups == 256, "one group to a thread");
     Codes<E, CODES ? NL : 1> k_codes, v_codes;
     auto request = [&](int half, int j) {
         const int n = j / (2 * NI), i = (j / 2) % NI;
         const uint32_t to = lds0 + (uint32_t)((half * kStepTiles + n) * STAGE + (i * NWAVES + w) * 1024);
         const Group& from_group = at[CODES ? 0 : n * NI + i];
-        if (j & 1) load_buffer_to_lds_16B(group_words(p.pages.v, from_group, token, E), from, to + TILE);
-        else load_buffer_to_lds_16B(group_words(p.pages.k, from_group, token, E), from, to);
+        if (j & 1) load_buffer_to_lds_16B(raw_buffer_words(static_cast<const uint8_t*>(p.pages.v) + from_group.at, from_group.bytes), from, to + TILE);
+        else load_buffer_to_lds_16B(raw_buffer_words(static_cast<const uint8_t*>(p.pages.k) + from_group.at, from_group.bytes), from, to);
     };
     static_assert(kStepTiles * NI * 2 == E / 16, "one transfer per group of score products");
     auto request_codes = [&]() {
@@ -447,7 +460,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     };
 
     if (walk.count > 0) {
-        fill_table(p, walk, s, 0, walk.count > kTableKeys ? 2 * kTableGroups : kTableGroups, groups);
+        fill_table(0);
+        if (walk.count > kTableKeys) fill_table(kTableKeys);
         wait_all_memory();                                // no wait for the queries inside the loop
         __syncthreads();
         next_step(0);
@@ -465,8 +479,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     auto arrived = [&](int n, int half) {
         if constexpr (CODES) lds_accesses_then_barrier();  // the codes stay under way
         else wait_all_memory(), __syncthreads();          // this step's tiles have landed for every wave; the other half is free
-        if (n % kTableKeys == 0 && n > 0 && n + kTableKeys < walk.count)
-            fill_table(p, walk, s, n + kTableKeys, kTableGroups, groups + (n / kTableKeys + 1) % 2 * kTableGroups);   // (many barriers before its first use)
+        if ((uint32_t)n % kTableKeys == 0 && n > 0 && n + kTableKeys < walk.count) fill_table(n + kTableKeys);   // (many barriers before its first use)
         if constexpr (CODES) {
             put_codes(half ^ 1);
             next_step(n + 2 * kStepKeys);
@@ -475,8 +488,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
             next_step(n + kStepKeys);
         }
     };
-    // The steps whose keys all of the wave's rows see, two at a time, whose LDS offsets are constants; and one by one those with hidden keys, and
-    // what is left over.  Waves may stand in different ones: each step of each is one barrier.
+    // The steps whose keys all of the wave's rows see, in two copies, whose LDS offsets are constants; then those with hidden keys.
+    // Waves may stand in different loops: each step of each is one barrier.
     uint32_t found = 0;
     auto step = [&](auto half_c, int n) {
         constexpr int half = decltype(half_c)::value;
@@ -491,79 +504,55 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
             tile_values<T, E, NQB, false>(st, S, vaddr, tile_off + TILE, p.sl2, found);
         }
     };
-    int moved = 0;                                        // where the addresses stand
-    auto hidden_step = [&](int n, int half) {
+    int n = 0;
+#pragma unroll 1
+    while (n + kStepKeys <= plain_end) {
+        step(std::integral_constant<int, 0>{}, n);
+        n += kStepKeys;
+        if (n + kStepKeys > plain_end) break;
+        step(std::integral_constant<int, 1>{}, n);
+        n += kStepKeys;
+    }
+    const int first_hidden = n;
+    int half = n / kStepKeys & 1;
+    auto move = [&](int bytes) {                          // the addresses to the other half
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
+    };
+    move(half * kStepTiles * STAGE);
+    auto nothing_seen = [&](int key) { return key >= seen || (key + kStepKeys <= low_of_any && key >= walk.sinks); };   // by this wave's rows
+#pragma unroll 1
+    for (; n < walk.count; n += kStepKeys, half ^= 1) {
         arrived(n, half);
         if constexpr (!CODES) {
 #pragma unroll
             for (int j = 0; j < E / 16; j++) request(half ^ 1, j);
         }
         const int key = walk.key(n);
-        if (key >= seen || (key + kStepKeys <= low_of_any && key >= walk.sinks)) return;   // nothing to see for this wave
-        const int bytes = (half - moved) * kStepTiles * STAGE;
-        moved = half;
+        if (!nothing_seen(key)) {
 #pragma unroll
-        for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
-#pragma unroll
-        for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
-#pragma unroll
-        for (int t = 0; t < kStepTiles; t++) {
-            f32x4 S[2][NQB];
-            tile_scores<T, E, NQB>(S, st, kaddr, t * STAGE, [](int) {});
-            hide_keys<NQB>(S, key + t * kTile + 4 * g, limit);
-            if (p.window) hide_far_keys<NQB>(S, key + t * kTile + 4 * g, low, walk.sinks);
-            raise_reference<T, E, NQB>(st, S, p.sl2, slack);
-            tile_values<T, E, NQB, true>(st, S, vaddr, t * STAGE + TILE, p.sl2, found);
-        }
-    };
-    auto is_plain = [&](int n) {
-        const int key = walk.key(n);
-        return n < walk.count && key + kStepKeys <= seen_by_all && (key >= low_of_all || key + kStepKeys <= walk.sinks);
-    };
-    auto goes_in_pairs = [&](int n, int half) { return half == 0 && is_plain(n) && is_plain(n + kStepKeys); };
-    int half = 0;
-#pragma unroll 1
-    for (int n = 0; n < walk.count;) {
-        if (goes_in_pairs(n, half)) {
-            if (moved) {
-                moved = 0;
-#pragma unroll
-                for (int es = 0; es < E / 32; es++) kaddr[es] -= kStepTiles * STAGE;
-#pragma unroll
-                for (int eb = 0; eb < E / 16; eb++) vaddr[eb] -= kStepTiles * STAGE;
+            for (int t = 0; t < kStepTiles; t++) {
+                f32x4 S[2][NQB];
+                tile_scores<T, E, NQB>(S, st, kaddr, t * STAGE, [](int) {});
+                hide_keys<NQB>(S, key + t * kTile + 4 * g, limit);
+                if (p.window) hide_far_keys<NQB>(S, key + t * kTile + 4 * g, low, walk.sinks);
+                raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+                tile_values<T, E, NQB, true>(st, S, vaddr, t * STAGE + TILE, p.sl2, found);
             }
-#pragma unroll 1
-            do {
-                step(std::integral_constant<int, 0>{}, n);
-                step(std::integral_constant<int, 1>{}, n + kStepKeys);
-                n += 2 * kStepKeys;
-            } while (goes_in_pairs(n, 0));
-        } else {
-            hidden_step(n, half);
-            n += kStepKeys;
-            half ^= 1;
         }
+        move(half ? -kStepTiles * STAGE : kStepTiles * STAGE);
     }
     wait_all_memory();                                    // the transfers behind the last step
 
-    // Infinite and NaN values among the steps that went one by one go to the queries that see them.
-    if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
-        half = 0;
+    // Infinite and NaN values among the steps with hidden keys go to the queries that see them.
+    if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
 #pragma unroll 1
-        for (int n = 0; n < walk.count;) {
-            if (goes_in_pairs(n, half)) {
-                n += 2 * kStepKeys;
-                continue;
-            }
-            const int key = walk.key(n);
-            if (key < seen && !(key + kStepKeys <= low_of_any && key >= walk.sinks))
-#pragma unroll 1
-                for (int t = 0; t < kStepTiles; t++)
-                    add_special_values<T, E, NQB, CODES>(st, p, s, kv_head, key + t * kTile, walk.end, walk.sinks, limit, low, g);
-            n += kStepKeys;
-            half ^= 1;
+        for (int at = first_hidden; at < walk.count; at += kTile) {
+            const int key = walk.key(at);
+            if (!nothing_seen(key / kStepKeys * kStepKeys)) add_special_values<T, E, NQB, CODES>(st, p, s, kv_head, key, walk.end, walk.sinks, limit, low, g);
         }
-    }
     store_rows<T, E, NQB>(st, limit, oh, p.out_token, w * NQB * 16, rows, g, l16);
 }
 
