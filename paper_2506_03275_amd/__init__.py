@@ -101,7 +101,7 @@ def _bind(lib):
         warnings.warn(f"the compiled binding is not used ({e}): calls take some 2 us longer (build() makes it anew)", RuntimeWarning)
         return _Python()
     names = ("voxel_reorder", "topk_cols", "attn_sparse_delta", "attn_dense", "attn_dense_colsum_stale", "mlp_tile_mean_preact",
-             "mlp_sparse_delta", "mlp_dense", "linear", "rope", "attn_packed", "norm_rope", "cache_write", "cache_read", "attn_paged")
+             "mlp_sparse_delta", "mlp_dense", "linear", "rope", "attn_packed", "norm_rope", "cache_write", "cache_read", "attn_paged", "norm_rope_grad")
     _native.bind({"chipmunk_" + n: ctypes.cast(getattr(lib, "chipmunk_" + n), _c_ptr).value for n in names}, _current_device, _raw_stream)
     return _native
 
@@ -536,6 +536,9 @@ def norm_rope_grad_workspace_bytes(tokens, heads, E):
 def norm_rope_grad(grad, x, q_weight, k_weight, q_heads, pos, freqs, dx, dq_weight, dk_weight, axes, eps=1e-6, halves=False, ws=None):
     """The gradient of norm_rope.  grad (of its result), x (as it had it), dx: [tokens, heads, E], any strides of tokens and heads, dx may be grad or x;
     dq_weight, dk_weight: fp32 [E]; ws: uint8 workspace of norm_rope_grad_workspace_bytes."""
+    status = _fast.norm_rope_grad(grad, x, q_weight, k_weight, q_heads, pos, freqs, dx, dq_weight, dk_weight, axes, eps, halves, ws)
+    if status is not None:
+        return _check(status, "chipmunk_norm_rope_grad")
     px, pd, pq, pk, q_heads, pp, pf, axes, number = _norm_arguments(x, q_weight, k_weight, q_heads, pos, freqs, dx, axes)
     pg, pws = _strided(grad, x.dtype, "grad", 3), _strided(ws, torch.uint8, "ws", 1, most=2 ** 63 - 1)
     pdq, pdk = _strided(dq_weight, torch.float32, "dq_weight", 1), _strided(dk_weight, torch.float32, "dk_weight", 1)

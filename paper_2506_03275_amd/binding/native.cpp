@@ -24,8 +24,8 @@ Entry entries[] = {{"chipmunk_voxel_reorder", nullptr},       {"chipmunk_topk_co
                    {"chipmunk_linear", nullptr},              {"chipmunk_rope", nullptr},
                    {"chipmunk_attn_packed", nullptr},         {"chipmunk_norm_rope", nullptr},
                    {"chipmunk_cache_write", nullptr},         {"chipmunk_cache_read", nullptr},
-                   {"chipmunk_attn_paged", nullptr}};
-enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense, kLinear, kRope, kAttnPacked, kNormRope, kCacheWrite, kCacheRead, kAttnPaged };
+                   {"chipmunk_attn_paged", nullptr},          {"chipmunk_norm_rope_grad", nullptr}};
+enum { kReorder, kTopk, kAttnDelta, kAttnDense, kAttnRefresh, kScores, kMlpDelta, kMlpDense, kLinear, kRope, kAttnPacked, kNormRope, kCacheWrite, kCacheRead, kAttnPaged, kNormRopeGrad };
 PyObject* current_device = nullptr;   // torch's functions that name the current device and, for a device, its current stream
 PyObject* raw_stream = nullptr;
 
@@ -411,6 +411,31 @@ PyObject* norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// grad, x, q_weight, k_weight, q_heads, pos, freqs, dx, dq_weight, dk_weight, axes, eps, halves, ws
+PyObject* norm_rope_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return answer(kNormRopeGrad, args, n, 14, [](Args& a, auto run) {
+        Strided s(a, 1);
+        const at::Tensor *grad = s.elements(0, 3), *x = s.elements(1, 3), *wq = s.optional(2, 1, s.element), *wk = s.optional(3, 1, s.element), *pos = s.optional(5, 2, at::kInt),
+                         *freqs = s.optional(6, 1, at::kDouble), *dx = s.elements(7, 3), *dq = s.optional(8, 1, at::kFloat), *dk = s.optional(9, 1, at::kFloat),
+                         *ws = s.optional(13, 1, at::kByte);
+        const int q_heads = a.integer(4);
+        const Axes axes(a, 10);
+        const float eps = a.real(11);
+        const bool halves = s.truth(12);
+        if (!a.ok || dx->sizes() != x->sizes() || grad->sizes() != x->sizes() || (wq && wq->size(0) != x->size(2)) || (wk && wk->size(0) != x->size(2)) ||
+            (dq && dq->size(0) != x->size(2)) || (dk && dk->size(0) != x->size(2)) || (pos && (pos->size(0) != x->size(0) || pos->size(1) != 3 || !pos->is_contiguous())) ||
+            (freqs && freqs->size(0) != axes.pairs())) {
+            a.ok = false;
+            return;
+        }
+        void* stream = a.stream();
+        run(decltype(&chipmunk_norm_rope_grad){}, elements_of(grad), grad->stride(0), grad->stride(1), elements_of(x), x->stride(0), x->stride(1), elements_of(wq), elements_of(wk),
+            q_heads, pos ? (const int32_t*)pos->data_ptr() : nullptr, freqs ? (const double*)freqs->data_ptr() : nullptr, const_cast<uint16_t*>(elements_of(dx)), dx->stride(0),
+            dx->stride(1), dq ? (float*)dq->data_ptr() : nullptr, dk ? (float*)dk->data_ptr() : nullptr, (int)x->size(0), (int)x->size(1), (int)x->size(2), axes.t, axes.h, axes.w,
+            eps, (int)halves, s.number(), ws ? ws->data_ptr() : nullptr, ws ? (size_t)ws->numel() : (size_t)0, stream);
+    });
+}
+
 // What a Pages object says of itself: the address of its struct, its device, heads and E
 struct PagesArg {
     const chipmunk_pages* at = nullptr;
@@ -499,7 +524,7 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(voxel_reorder), FAST(topk_cols), FAST(attn_sparse_delta), FAST(attn_dense),
                          FAST(attn_dense_colsum_stale), FAST(mlp_tile_mean_preact), FAST(mlp_sparse_delta), FAST(mlp_dense),
-                         FAST(linear), FAST(rope), FAST(attn_packed), FAST(norm_rope), FAST(cache_write), FAST(cache_read), FAST(attn_paged),
+                         FAST(linear), FAST(rope), FAST(attn_packed), FAST(norm_rope), FAST(cache_write), FAST(cache_read), FAST(attn_paged), FAST(norm_rope_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -174,10 +174,11 @@ __device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, cons
 // Few queries over many keys, as attn_packed_few_kernel: a workgroup owns one key head of one sequence and walks part_keys of its numbered keys for
 // block_rows rows of the head; its waves take the tiles of 32 keys in turn and meet at the end.
 template <class T, int E, int NQB, bool CODES>
-__global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(PagedParams p) {
+__global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void attn_paged_few_kernel(PagedParams p) {
     typedef typename T::x8 x8;
     constexpr int ROWB = E * 2, CH = ROWB / 16, RPI = 64 / CH, NI = kTile / RPI;   // NI: transfers of a tile
-    constexpr int TILE = kTile * ROWB, NL = kTile * E / 1024;                      // NL: loads of a tile's codes
+    constexpr int NL = kTile * E / 1024;                  // loads of a tile's codes
+    constexpr int TILE = kTile * ROWB, TILES = CODES ? 1 : 2, V_TILE = (TILES - 1) * TILE;   // of codes K and V go through one tile by turns
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     __shared__ u32x4 places[4][kWave];                    // of each wave's next 32 tiles' groups
     __shared__ u32x2 scale_places[CODES ? 4 : 1][kWave];
@@ -194,6 +195,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
     const int keys = keys_held(p, s), past = keys - qs.count;
     const int i0 = row0 / p.G, i1 = (row0 + rows - 1) / p.G;
     const Walk walk = walk_of<kTile>(p, i0, i1, keys, past);
+    const int low_of_all = low_of(p, i1, past);
     const int64_t start64 = (int64_t)part * p.part_keys;
     if (start64 >= walk.count && part > 0) return;        // (without any key the first part writes zeros)
     const int start = (int)start64, end = (int)std::min<int64_t>(walk.count, start64 + p.part_keys);
@@ -221,13 +223,13 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
     const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
     const int vrow = 4 * g + (l16 >> 2);
     const int voff = vrow * ROWB + ((((l16 & 3) >> 1) ^ tile_swizzle<E>(vrow)) * 16) + 8 * (l16 & 1);
-    const uint32_t smem_at = (uint32_t)(uintptr_t)CHIPMUNK_LDS_PTR(smem) + w * 2 * TILE;
+    const uint32_t smem_at = (uint32_t)(uintptr_t)CHIPMUNK_LDS_PTR(smem) + w * TILES * TILE;
     uint32_t kaddr[E / 32], vaddr[E / 16];
 #pragma unroll
     for (int es = 0; es < E / 32; es++) kaddr[es] = smem_at + (uint32_t)(koff ^ (64 * es));
 #pragma unroll
     for (int eb = 0; eb < E / 16; eb++) vaddr[eb] = smem_at + (uint32_t)(voff ^ (32 * eb));
-    const uint32_t lds0 = lds_address(smem) + (uint32_t)(w * 2 * TILE);
+    const uint32_t lds0 = lds_address(smem) + (uint32_t)(w * TILES * TILE);
     const int64_t token = p.pages.token_stride;
     constexpr int NIG = NI / 2;                           // transfers of a group: a lane's offsets into it stay the same
     uint32_t from[NIG];
@@ -273,7 +275,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
         if ((uint32_t)(n - first) % (kWave / 2 * TURN) == 0 && n < end) fill_table(n);
         request(p.pages.k, p.pages.k_scales, k_codes, n, lds0);
     };
-    auto request_v = [&](int n) { request(p.pages.v, p.pages.v_scales, v_codes, n, lds0 + TILE); };
+    auto request_v = [&](int n) { request(p.pages.v, p.pages.v_scales, v_codes, n, lds0 + V_TILE); };
     uint32_t found = 0;
     int n = first;
     auto tile = [&](auto hidden_c) {
@@ -294,17 +296,17 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
         if (HIDDEN) {
             const int key = walk.key(n);
             hide_keys<NQB>(S, key + 4 * g, limit);
-            if (p.window) hide_far_keys<NQB>(S, key + 4 * g, low, walk.sinks);
+            if (key < low_of_all) hide_far_keys<NQB>(S, key + 4 * g, low, walk.sinks);
         }
         raise_reference<T, E, NQB>(st, S, p.sl2, slack);
         if constexpr (CODES) {
-            put(v_codes, lds0 + TILE);
+            put(v_codes, lds0 + V_TILE);
             request_v(n + TURN);
         } else {
             wait_vmem_at_most<NI>();                      // V
             asm volatile("" ::: "memory");
         }
-        tile_values<T, E, NQB, HIDDEN>(st, S, vaddr, TILE, p.sl2, found);
+        tile_values<T, E, NQB, HIDDEN>(st, S, vaddr, V_TILE, p.sl2, found);
         if constexpr (!CODES) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             request_v(n + TURN);
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : 2) void attn_paged_few_kernel(P
 // two tiles of 32.  Elements go from the pages to LDS by asynchronous loads, double buffered by step; codes are in registers a step before, and go to LDS
 // as elements while the step before theirs is computed.
 template <class T, int E, int NQB, bool CODES>
-__global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) {
+__global__ __launch_bounds__(256, E == 64 && NQB <= 2 ? 3 : 2) void attn_paged_rows_kernel(PagedParams p) {
     typedef typename T::x8 x8;
     constexpr int NWAVES = 4, ROWS = 16 * NQB * NWAVES;
     constexpr int ROWB = E * 2;                           // bytes per K/V row of a tile
@@ -387,7 +389,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     const int wave_row = w * NQB * 16, wave_rows = min(rows - wave_row, NQB * 16);
     const int first_row = row0 + wave_row, last_row = first_row + max(wave_rows, 1) - 1;
     const int seen = wave_rows <= 0 ? 0 : limit_of(p, last_row, keys, past), low_of_any = low_of(p, first_row, past);
-    const int plain_end = wave_rows <= 0 ? 0 : min(walk.upto, limit_of(p, first_row, keys, past) - walk.high);
+    const int seen_by_all = wave_rows <= 0 ? 0 : limit_of(p, first_row, keys, past), low_of_all = low_of(p, last_row, past);
+    const int plain_end = min(walk.upto, seen_by_all - walk.high);
     const float slack = kSlack / p.sl2;
 
     const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
@@ -427,7 +430,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
         if (CODES) scale_places[CODES ? i : 0] = to.scales;
     };
     static_assert(kTableGroups == 256, "one group to a thread");
-    Codes<E, CODES ? NL : 1> k_codes, v_codes;
+    // Codes of the next SETS steps are under way: a step of narrow heads is shorter than memory takes; wide ones have no registers for two.
+    constexpr int SETS = CODES && E == 64 ? 2 : 1;
+    Codes<E, CODES ? NL : 1> k_codes[SETS], v_codes[SETS];
     auto request = [&](int half, int j) {
         const int n = j / (2 * NI), i = (j / 2) % NI;
         const uint32_t to = lds0 + (uint32_t)((half * kStepTiles + n) * STAGE + (i * NWAVES + w) * 1024);
@@ -436,28 +441,32 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
         else load_buffer_to_lds_16B(raw_buffer_words(static_cast<const uint8_t*>(p.pages.k) + from_group.at, from_group.bytes), from, to);
     };
     static_assert(kStepTiles * NI * 2 == E / 16, "one transfer per group of score products");
-    auto request_codes = [&]() {
+    auto request_codes = [&](auto set_c) {
         if constexpr (CODES) {
+            constexpr int set = decltype(set_c)::value % SETS;
 #pragma unroll
             for (int i = 0; i < NL; i++) {
-                k_codes.request(i, p, p.pages.k, p.pages.k_scales, at[i], in_group, lane);
-                v_codes.request(i, p, p.pages.v, p.pages.v_scales, at[i], in_group, lane);
+                k_codes[set].request(i, p, p.pages.k, p.pages.k_scales, at[i], in_group, lane);
+                v_codes[set].request(i, p, p.pages.v, p.pages.v_scales, at[i], in_group, lane);
             }
         }
     };
-    auto put_codes = [&](int half) {
+    auto put_codes = [&](auto set_c, int half) {
         if constexpr (CODES) {
+            constexpr int set = decltype(set_c)::value % SETS;
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int i = 0; i < NL; i++) {
                 const int row = group_at(i) * kGroup + in_group + lane / Codes<E, NL>::LANES;   // of the step
                 const uint32_t to = lds0 + (uint32_t)((half * kStepTiles + group_at(i) / 2) * STAGE);
-                k_codes.template put<T>(i, to, row % kTile, lane);
-                v_codes.template put<T>(i, to + TILE, row % kTile, lane);
+                k_codes[set].template put<T>(i, to, row % kTile, lane);
+                v_codes[set].template put<T>(i, to + TILE, row % kTile, lane);
             }
             asm volatile("" ::: "memory");
         }
     };
+    typedef std::integral_constant<int, 0> Even;
+    typedef std::integral_constant<int, 1> Odd;
 
     if (walk.count > 0) {
         fill_table(0);
@@ -466,24 +475,28 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
         __syncthreads();
         next_step(0);
         if constexpr (CODES) {
-            request_codes();
-            put_codes(0);
-            next_step(kStepKeys);
-            request_codes();
+            request_codes(Even{});
+            if (SETS == 2) {
+                next_step(kStepKeys);
+                request_codes(Odd{});
+            }
+            put_codes(Even{}, 0);
+            next_step(SETS * kStepKeys);
+            request_codes(std::integral_constant<int, SETS>{});
         } else {
 #pragma unroll
             for (int j = 0; j < E / 16; j++) request(0, j);
         }
     }
-    // Begins the step from numbered key n on, whose tiles are in half `half`.
-    auto arrived = [&](int n, int half) {
+    // Begins the step from numbered key n on, whose tiles are in half `half`.  (set: of the step behind it, whose parity is the other half's)
+    auto arrived = [&](auto set_c, int half, int n) {
         if constexpr (CODES) lds_accesses_then_barrier();  // the codes stay under way
         else wait_all_memory(), __syncthreads();          // this step's tiles have landed for every wave; the other half is free
         if ((uint32_t)n % kTableKeys == 0 && n > 0 && n + kTableKeys < walk.count) fill_table(n + kTableKeys);   // (many barriers before its first use)
         if constexpr (CODES) {
-            put_codes(half ^ 1);
-            next_step(n + 2 * kStepKeys);
-            request_codes();
+            put_codes(set_c, half ^ 1);
+            next_step(n + (SETS + 1) * kStepKeys);
+            request_codes(set_c);
         } else {
             next_step(n + kStepKeys);
         }
@@ -493,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
     uint32_t found = 0;
     auto step = [&](auto half_c, int n) {
         constexpr int half = decltype(half_c)::value;
-        arrived(n, half);
+        arrived(std::integral_constant<int, half ^ 1>{}, half, n);
 #pragma unroll
         for (int t = 0; t < kStepTiles; t++) {
             const int tile_off = (half * kStepTiles + t) * STAGE;
@@ -504,45 +517,60 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedParams p) 
             tile_values<T, E, NQB, false>(st, S, vaddr, tile_off + TILE, p.sl2, found);
         }
     };
-    int n = 0;
-#pragma unroll 1
-    while (n + kStepKeys <= plain_end) {
-        step(std::integral_constant<int, 0>{}, n);
-        n += kStepKeys;
-        if (n + kStepKeys > plain_end) break;
-        step(std::integral_constant<int, 1>{}, n);
-        n += kStepKeys;
-    }
-    const int first_hidden = n;
-    int half = n / kStepKeys & 1;
-    auto move = [&](int bytes) {                          // the addresses to the other half
-#pragma unroll
-        for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
-#pragma unroll
-        for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
-    };
-    move(half * kStepTiles * STAGE);
     auto nothing_seen = [&](int key) { return key >= seen || (key + kStepKeys <= low_of_any && key >= walk.sinks); };   // by this wave's rows
-#pragma unroll 1
-    for (; n < walk.count; n += kStepKeys, half ^= 1) {
-        arrived(n, half);
+    auto hidden_step = [&](auto set_c, int half, int n, int base) {   // base: what the addresses lack
+        arrived(set_c, half, n);
         if constexpr (!CODES) {
 #pragma unroll
             for (int j = 0; j < E / 16; j++) request(half ^ 1, j);
         }
         const int key = walk.key(n);
-        if (!nothing_seen(key)) {
+        if (nothing_seen(key)) return;
 #pragma unroll
-            for (int t = 0; t < kStepTiles; t++) {
-                f32x4 S[2][NQB];
-                tile_scores<T, E, NQB>(S, st, kaddr, t * STAGE, [](int) {});
-                hide_keys<NQB>(S, key + t * kTile + 4 * g, limit);
-                if (p.window) hide_far_keys<NQB>(S, key + t * kTile + 4 * g, low, walk.sinks);
-                raise_reference<T, E, NQB>(st, S, p.sl2, slack);
-                tile_values<T, E, NQB, true>(st, S, vaddr, t * STAGE + TILE, p.sl2, found);
-            }
+        for (int t = 0; t < kStepTiles; t++) {
+            f32x4 S[2][NQB];
+            tile_scores<T, E, NQB>(S, st, kaddr, base + t * STAGE, [](int) {});
+            if (key + kStepKeys > seen_by_all) hide_keys<NQB>(S, key + t * kTile + 4 * g, limit);
+            if (key < low_of_all) hide_far_keys<NQB>(S, key + t * kTile + 4 * g, low, walk.sinks);
+            raise_reference<T, E, NQB>(st, S, p.sl2, slack);
+            tile_values<T, E, NQB, true>(st, S, vaddr, base + t * STAGE + TILE, p.sl2, found);
         }
-        move(half ? -kStepTiles * STAGE : kStepTiles * STAGE);
+    };
+    // (codes: an even number, so that the steps behind them are in pairs as well, which takes fewer registers)
+    const int plain_keys = CODES ? plain_end / (2 * kStepKeys) * (2 * kStepKeys) : plain_end;
+    int n = 0;
+#pragma unroll 1
+    while (n + kStepKeys <= plain_keys) {
+        step(Even{}, n);
+        n += kStepKeys;
+        if (n + kStepKeys > plain_keys) break;
+        step(Odd{}, n);
+        n += kStepKeys;
+    }
+    const int first_hidden = n;
+    if constexpr (CODES) {
+#pragma unroll 1
+        while (n < walk.count) {
+            hidden_step(Odd{}, 0, n, 0);
+            n += kStepKeys;
+            if (n >= walk.count) break;
+            hidden_step(Even{}, 1, n, kStepTiles * STAGE);
+            n += kStepKeys;
+        }
+    } else {
+        auto move = [&](int bytes) {                      // the addresses to the other half
+#pragma unroll
+            for (int es = 0; es < E / 32; es++) kaddr[es] += bytes;
+#pragma unroll
+            for (int eb = 0; eb < E / 16; eb++) vaddr[eb] += bytes;
+        };
+        int half = n / kStepKeys & 1;
+        move(half * kStepTiles * STAGE);
+#pragma unroll 1
+        for (; n < walk.count; n += kStepKeys, half ^= 1) {
+            hidden_step(Even{}, half, n, 0);
+            move(half ? -kStepTiles * STAGE : kStepTiles * STAGE);
+        }
     }
     wait_all_memory();                                    // the transfers behind the last step
 
@@ -593,7 +621,7 @@ static int32_t launch_paged_rows(PagedParams p, hipStream_t stream) {
 template <class T, int E, int NQB, bool CODES>
 static int32_t launch_paged_few(PagedParams p, hipStream_t stream) {
     constexpr int TOGETHER = NQB < 2 ? NQB : 2;
-    constexpr int LDS = std::max(4 * 2 * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
+    constexpr int LDS = std::max(4 * (CODES ? 1 : 2) * kTile * E * 2, 4 * TOGETHER * (E * 64 + 512));
     const auto kernel = attn_paged_few_kernel<T, E, NQB, CODES>;
     const PackedGrid grid = few_grid(16 * NQB, p.S, p.Hk, p.few_rows, p.parts);
     if (grid.workgroups >= kMostWorkgroups) return CHIPMUNK_ERR_SHAPE;

@@ -5,6 +5,8 @@
 #include "pages.h"
 #include "rope.h"
 
+#include <type_traits>
+
 namespace chipmunk {
 
 struct CacheParams {
@@ -29,7 +31,11 @@ struct CacheItem {
 };
 __device__ __forceinline__ CacheItem cache_item(const CacheParams& p) {
     const uint32_t per_row = p.pages.E / 16, per_token = per_row * 2 * p.pages.heads;
-    const int64_t id = (int64_t)blockIdx.x * kCacheThreads + threadIdx.x;
+    // Workgroups go to the eight XCDs in turn: each XCD takes one run of the tokens, so that the scales of neighbouring tokens, bytes of one line,
+    // meet in one L2
+    const uint32_t run = gridDim.x / 8, more = gridDim.x % 8, xcd = blockIdx.x % 8;
+    const uint32_t block = xcd * run + min(xcd, more) + blockIdx.x / 8;
+    const int64_t id = (int64_t)block * kCacheThreads + threadIdx.x;
     const int64_t token = id / per_token;
     const uint32_t in_token = (uint32_t)(id - token * per_token), row = in_token / per_row;
     return CacheItem{token, (int)(row % p.pages.heads), (int)(in_token % per_row), row >= (uint32_t)p.pages.heads};
@@ -40,7 +46,8 @@ __device__ __forceinline__ int64_t place_of(const CacheParams& p, int64_t row, i
     return (row >> p.shift) * page_stride + (row & (p.pages.page_size - 1)) * token_stride + head * head_stride;
 }
 
-template <class T, bool CODES>
+// FAR: new tokens beyond the L2s pass them by (rope.h; 67 MB 45 -> 39 us with the way back).
+template <class T, bool CODES, bool FAR>
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheParams p) {
     const CacheItem at = cache_item(p);
     if (at.token >= p.tokens) return;                // (with all threads of its row)
@@ -49,7 +56,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheParams 
     const uint16_t* from = at.value ? p.from_v + at.token * p.v_token + at.head * p.v_head : p.from_k + at.token * p.k_token + at.head * p.k_head;
     u32x4 x[2];
 #pragma unroll
-    for (int i = 0; i < 2; i++) x[i] = reinterpret_cast<const u32x4*>(from + at.chunk * 16)[i];
+    for (int i = 0; i < 2; i++) x[i] = rope_load<FAR ? kPastL2 : kThroughCaches>(from + at.chunk * 16 + i * 8);
     const int64_t to = place_of(p, row, at.head, p.pages.page_stride, p.pages.token_stride, p.pages.head_stride) + at.chunk * 16;
     void* held = at.value ? p.pages.v : p.pages.k;
     if constexpr (!CODES) {
@@ -58,43 +65,50 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheParams 
         return;
     }
     typedef Magnitudes<T> M;
-    // By the bits: the order of the magnitudes is that of their 15 bits, and these files are compiled as if NaN did not exist.
-    uint32_t most = 0;
-    uint32_t mag[16], sign[16];
+    // The order of the magnitudes is that of their 15 bits, two to a word; over the row's threads: 4 (E = 64) or 8 side by side.
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    const bool eight = p.pages.E == 128;
+    auto row_most = [&]() {
+        u16x2 most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const uint32_t bits = i % 2 ? x[i / 8][i % 8 / 2] >> 16 : x[i / 8][i % 8 / 2] & 0xffffu;
-        mag[i] = bits & 0x7fffu;
-        sign[i] = bits & 0x8000u;
-        const bool finite = mag[i] < M::kNotFinite;
-        if (finite) mag[i] = min(mag[i], M::kMost);
-        most = max(most, finite ? mag[i] : 0u);
+        for (int i = 0; i < 8; i++) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[i / 4][i % 4] & 0x7fff7fffu));
+        uint32_t m = max((uint32_t)most[0], (uint32_t)most[1]);
+        m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, false));         // quad_perm 1 0 3 2
+        m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, false));         // quad_perm 2 3 0 1
+        if (eight) m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, false));   // row_half_mirror
+        return m;
+    };
+    uint32_t most = row_most();
+    uint32_t special = 0;                            // a bit for each element that is infinite or NaN
+    if (most > M::kMost) {                           // (a row's threads alike) those out of the way, and magnitudes beyond the most cut
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const int at = i % 2 * 16;
+            const uint32_t bits = x[i / 8][i % 8 / 2] >> at & 0xffffu, magnitude = bits & 0x7fffu;
+            if (magnitude <= M::kMost) continue;
+            const bool finite = magnitude < M::kNotFinite;
+            if (!finite) special |= 1u << i;
+            x[i / 8][i % 8 / 2] = (x[i / 8][i % 8 / 2] & ~(0xffffu << at)) | (finite ? (bits & 0x8000u) | M::kMost : 0u) << at;
+        }
+        most = row_most();
     }
-    // over the row's threads: 4 (E = 64) or 8 side by side
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, false));        // quad_perm 1 0 3 2
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4e, 0xf, 0xf, false));        // quad_perm 2 3 0 1
-    if (p.pages.E == 128) most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x141, 0xf, 0xf, false));   // row_half_mirror
     const int k = e4m3_exponent(__float_as_uint(T::low(most)));
-    const float down = power_of_two(-k);
+    const float power = power_of_two(k);
     u32x4 codes;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        float f[4];
+    for (int i = 0; i < 4; i++) codes[i] = codes_of_elements<T, true>(x[i / 2][i % 2 * 2 + 1], codes_of_elements<T, false>(x[i / 2][i % 2 * 2], 0u, power), power);
+    if (special) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint32_t m = mag[4 * i + j];
-            // no finite value passes 448; the others become NaN, which the conversion leaves NaN
-            f[j] = __uint_as_float(m < M::kNotFinite ? __float_as_uint(T::low(m | sign[4 * i + j]) * down) : 0x7fc00000u);
-        }
-        const int half = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-        codes[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], half, true);
+        for (int i = 0; i < 16; i++)
+            if (special >> i & 1) codes[i / 4] |= 0x7fu << i % 4 * 8;
     }
     *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(held) + to) = codes;
     if (at.chunk == 0)
         (at.value ? p.pages.v_scales : p.pages.k_scales)[place_of(p, row, at.head, p.pages.scale_page_stride, p.pages.scale_token_stride, p.pages.scale_head_stride)] = (uint8_t)(k + 127);
 }
 
-template <class T, bool CODES>
+// RESULT: one beyond the last-level cache passes it by.
+template <class T, bool CODES, int RESULT>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheParams p) {
     const CacheItem at = cache_item(p);
     if (at.token >= p.tokens) return;
@@ -119,7 +133,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheParams p
     }
     uint16_t* to = (at.value ? p.to_v + at.token * p.v_token + at.head * p.v_head : p.to_k + at.token * p.k_token + at.head * p.k_head) + at.chunk * 16;
 #pragma unroll
-    for (int i = 0; i < 2; i++) reinterpret_cast<u32x4*>(to)[i] = x[i];
+    for (int i = 0; i < 2; i++) rope_store<RESULT>(raw_buffer(to, 0), to, to + i * 8, x[i]);
 }
 
 // The checks that writing and reading share.
@@ -153,9 +167,13 @@ extern "C" int32_t chipmunk_cache_write(const uint16_t* k, int64_t k_token_strid
     if (status != CHIPMUNK_OK) return status;
     const auto s = static_cast<hipStream_t>(stream);
     const uint32_t grid = cache_workgroups(p);
-    if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_write_kernel<Bf16, false><<<grid, kCacheThreads, 0, s>>>(p);   // (a copy is a copy)
-    else if (dtype == CHIPMUNK_DTYPE_BF16) cache_write_kernel<Bf16, true><<<grid, kCacheThreads, 0, s>>>(p);
-    else cache_write_kernel<Fp16, true><<<grid, kCacheThreads, 0, s>>>(p);
+    auto go = [&](auto far) {
+        constexpr bool FAR = decltype(far)::value;
+        if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_write_kernel<Bf16, false, FAR><<<grid, kCacheThreads, 0, s>>>(p);   // (a copy is a copy)
+        else if (dtype == CHIPMUNK_DTYPE_BF16) cache_write_kernel<Bf16, true, FAR><<<grid, kCacheThreads, 0, s>>>(p);
+        else cache_write_kernel<Fp16, true, FAR><<<grid, kCacheThreads, 0, s>>>(p);
+    };
+    (int64_t)tokens * p.pages.heads * p.pages.E * 4 > kRopeL2 ? go(std::true_type{}) : go(std::false_type{});
     return launch_status();
 }
 
@@ -167,8 +185,13 @@ extern "C" int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_
     if (status != CHIPMUNK_OK) return status;
     const auto s = static_cast<hipStream_t>(stream);
     const uint32_t grid = cache_workgroups(p);
-    if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_read_kernel<Bf16, false><<<grid, kCacheThreads, 0, s>>>(p);
-    else if (dtype == CHIPMUNK_DTYPE_BF16) cache_read_kernel<Bf16, true><<<grid, kCacheThreads, 0, s>>>(p);
-    else cache_read_kernel<Fp16, true><<<grid, kCacheThreads, 0, s>>>(p);
+    auto go = [&](auto result) {
+        constexpr int RESULT = decltype(result)::value;
+        if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_read_kernel<Bf16, false, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
+        else if (dtype == CHIPMUNK_DTYPE_BF16) cache_read_kernel<Bf16, true, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
+        else cache_read_kernel<Fp16, true, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
+    };
+    if ((int64_t)tokens * p.pages.heads * p.pages.E * 4 > kRopeLastLevel) go(std::integral_constant<int, kPastLastLevel>{});
+    else go(std::integral_constant<int, kKept>{});
     return launch_status();
 }

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p) {
 template <class T, bool HALVES, int SOURCE, int RESULT>
 __global__ __launch_bounds__(kNormThreads) void norm_rope_grad_kernel(NormParams p) {
     typedef NormItem<T, HALVES> Item;
-    __shared__ float sums[kNormThreads * Item::NE];
+    __shared__ float sums[2][kNormThreads * Item::NE];   // of either weight, [slot][element]
     const int slot = threadIdx.x / p.lanes, item = threadIdx.x & (p.lanes - 1);
     const int in_group = slot / p.side, first_head = (int)blockIdx.y * p.side * p.per + slot - in_group * p.side;
     const Item it(p, item);
@@ -247,64 +247,78 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_grad_kernel(NormParams
             }
         }
     }
-    // the rows that the workgroup's threads have side by side: sums[slot][element]
-    float* mine = p.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.E;
-    const int slots = kNormThreads / p.lanes;
+    // the rows that the workgroup's threads have side by side
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        __syncthreads();
+    for (int i = 0; i < 2; i++)
         if (it.present) {
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                sums[slot * p.E + it.e0 + e] = dw[i][e];
-                if (HALVES && it.turn) sums[slot * p.E + it.e1 + e] = dw[i][Item::NE - 8 + e];
+                sums[i][slot * p.E + it.e0 + e] = dw[i][e];
+                if (HALVES && it.turn) sums[i][slot * p.E + it.e1 + e] = dw[i][Item::NE - 8 + e];
             }
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < p.E; e += kNormThreads) {
-            float sum = 0.f;
-            for (int n = 0; n < slots; n++) sum += sums[n * p.E + e];
-            mine[i * p.E + e] = sum;
-        }
+    __syncthreads();
+    float* mine = p.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.E;
+    const int slots = kNormThreads / p.lanes;
+    for (int e = threadIdx.x; e < 2 * p.E; e += kNormThreads) {
+        const float* column = e < p.E ? sums[0] + e : sums[1] + e - p.E;
+        float sum = 0.f;
+#pragma unroll 8
+        for (int n = 0; n < slots; n++) sum += column[n * p.E];
+        mine[e] = sum;
     }
 }
 
-// The workgroups' sums joined: 16 columns to a workgroup, 16 threads to a column.
-__global__ __launch_bounds__(256) void norm_weights_kernel(const float* partial, int workgroups, int E, float* dq, float* dk) {
-    __shared__ float sums[16][16];
-    const int column = threadIdx.x & 15, lane = threadIdx.x >> 4, at = (int)blockIdx.x * 16 + column;
+// The workgroups' sums joined: 16 columns to a workgroup, 64 threads to a column with eight sums each under way.
+__global__ __launch_bounds__(1024) void norm_weights_kernel(const float* partial, int workgroups, int E, float* dq, float* dk) {
+    __shared__ float sums[64][16];
+    const int column = threadIdx.x & 15, lane = threadIdx.x >> 4, at = min((int)blockIdx.x * 16 + column, 2 * E - 1);
     float sum = 0.f;
-    if (at < 2 * E)
-        for (int n = lane; n < workgroups; n += 16) sum += partial[(int64_t)n * 2 * E + at];
+    for (int n0 = lane; n0 < workgroups; n0 += 512) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = partial[(int64_t)min(n0 + i * 64, workgroups - 1) * 2 * E + at];
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += n0 + i * 64 < workgroups ? v[i] : 0.f;
+    }
     sums[lane][column] = sum;
     __syncthreads();
-    if (lane > 0 || at >= 2 * E) return;
+    if (lane > 0 || (int)blockIdx.x * 16 + column >= 2 * E) return;
 #pragma unroll
-    for (int n = 1; n < 16; n++) sum += sums[n][column];
+    for (int n = 1; n < 64; n++) sum += sums[n][column];
     float* to = at < E ? dq : dk;
     if (to) to[at < E ? at : at - E] = sum;
 }
+
+// Workgroups of the gradient at most: as many sums of weights are joined.
+constexpr int64_t kNormGradWorkgroups = 2048;
+constexpr int kNormGradMost = 12;    // heads of a thread
 
 // How a launch's threads are laid out: rows of a token side by side; a result in heads of rows gets four tokens' rows in one run (rope.hip).
 struct NormGrid {
     int items, lanes, side, per, at_once, parts;
     int64_t groups;          // of tokens
 };
-static NormGrid norm_grid(int tokens, int heads, int E, int64_t pairs, bool halves, bool heads_of_rows, int per) {
+static NormGrid norm_grid(int tokens, int heads, int E, int64_t pairs, bool halves, bool heads_of_rows, bool grad) {
     NormGrid g;
+    int per = grad ? kNormGradAhead : kNormAhead;
     g.items = halves ? (int)(pairs / 8 + (E - 2 * pairs) / 8) : E / 8;
     g.lanes = 1;
     while (g.lanes < g.items) g.lanes *= 2;
     const int slots = kNormThreads / g.lanes;
-    g.per = per;
     g.side = std::min(heads_of_rows ? std::min(4, slots) : slots, (heads + per - 1) / per);
+    // The gradient's angles serve more heads of a thread where there are workgroups enough: as many as divide the heads best
+    if (grad && (int64_t)tokens * heads / (slots * kNormGradMost) >= kNormGradWorkgroups) {
+        auto over = [&](int n) { return (heads + g.side * n - 1) / (g.side * n) * g.side * n; };
+        for (int n = per; n <= kNormGradMost; n += kNormGradAhead)
+            if (over(n) <= over(per)) per = n;
+    }
+    g.per = per;
     g.at_once = slots / g.side;
     g.parts = (heads + g.side * per - 1) / (g.side * per);
     g.groups = ((int64_t)tokens + g.at_once - 1) / g.at_once;
     return g;
 }
-// Workgroups of the gradient at most: as many sums of weights are joined.
-constexpr int64_t kNormGradWorkgroups = 1024;
 
 template <class T, bool HALVES>
 static void norm_launch(const NormParams& p, bool grad, dim3 grid, int source, int result, hipStream_t s) {
@@ -344,7 +358,7 @@ static int32_t norm_call(NormParams& p, bool grad, int64_t pairs_t, int64_t pair
     p.end1 = (int)(pairs_t + pairs_h);
     p.pairs = (int)pairs;
     p.inv_E = 1.f / (float)p.E;
-    const NormGrid g = norm_grid(p.tokens, p.heads, p.E, pairs, halves != 0, p.out_head > p.out_token, grad ? kNormGradAhead : kNormAhead);
+    const NormGrid g = norm_grid(p.tokens, p.heads, p.E, pairs, halves != 0, p.out_head > p.out_token, grad);
     p.items = g.items;
     p.lanes = g.lanes;
     p.side = g.side;
@@ -404,6 +418,6 @@ extern "C" int32_t chipmunk_norm_rope_grad(const uint16_t* grad, int64_t grad_to
     const auto s = static_cast<hipStream_t>(stream);
     status = norm_call(p, true, pairs_t, pairs_h, pairs_w, halves, dtype, grid, nullptr, s);
     if (status != CHIPMUNK_OK) return status;
-    norm_weights_kernel<<<(2 * E + 15) / 16, 256, 0, s>>>(p.partial, workgroups, E, dq_weight, dk_weight);
+    norm_weights_kernel<<<(2 * E + 15) / 16, 1024, 0, s>>>(p.partial, workgroups, E, dq_weight, dk_weight);
     return launch_status();
 }

@@ -34,6 +34,16 @@ template <> __device__ __forceinline__ u32x2 elements_of_codes<Fp16>(uint32_t co
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true))};
 }
 
+// Two elements under a power of two as codes, in half `upper` of a word: exact up to the one rounding, to nearest even.  (Of magnitudes above 448 times the
+// power it makes NaN.)
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+template <class T, bool upper> __device__ __forceinline__ uint32_t codes_of_elements(uint32_t word, uint32_t into, float scale) {
+    if constexpr (T::kOnes == Bf16::kOnes)
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(__builtin_bit_cast(s16x2, into), __builtin_bit_cast(bf16x2, word), scale, upper));
+    else
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(__builtin_bit_cast(s16x2, into), __builtin_bit_cast(fp16x2, word), scale, upper));
+}
+
 // ---- host side ---------------------------------------------------------------
 
 // What is wrong with the pages of a call whose elements are of type dtype.  A stride along a size of one becomes zero.
