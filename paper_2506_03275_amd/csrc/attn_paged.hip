@@ -600,11 +600,45 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(PagedParams p) {
     join_parts<T, E>(p, s, head, row, qs.first, min((walk.count - 1) / p.part_keys + 1, p.parts), limit_of(p, row / p.G, keys, past) > 0, lane);
 }
 
-// The numbered keys that a workgroup has at most: its rows' queries, at most max_q of them, see as many more than a window, in steps of `step`.
-static int most_numbered(int max_q, int max_k, int window, int sinks, int step) {
+// The numbered keys that a workgroup has at most: its rows' queries, at most max_q of them, see as many more than a window, in whole steps.
+static int most_numbered(int max_q, int max_k, int window, int sinks) {
     if (window == 0) return max_k;
-    const int64_t most = (int64_t)window + max_q + sinks + 2 * step;
+    const int64_t most = (int64_t)window + max_q + sinks + 2 * kStepKeys;
     return (int)std::min<int64_t>(most, max_k);
+}
+
+// Up to 32 rows of a key head: parts of so many of n numbered keys, as few_plan has them, or whole sequences (rows 0).  A part of codes costs half as
+// many keys' time to begin and end, and three workgroups stand on a CU; of elements two, and more than one and less than eight workgroups to a
+// CU leave some without work.  Measured on 4009 batches of 1 to 128 sequences, 300 to 40 000 keys, ragged and not: the length taken
+// takes 1.03 times the quickest's time in the mean (as few_plan has it 1.06 of codes, 1.04 of elements).
+static FewPlan paged_plan(int S, int Hq, int Hk, int max_q, int n, bool codes) {
+    const int64_t rows = (int64_t)max_q * (Hq / Hk), heads = (int64_t)S * Hk;
+    if (rows > 32 || heads > kMostPartWorkgroups / 2) return few_plan(S, Hq, Hk, max_q, n);
+    if (n <= (codes ? std::min<int64_t>(700 + 4 * heads, 3000) : std::min<int64_t>(1000 + 15 * heads, 3000))) return FewPlan{0, 0, 0};
+    int keys = 0;
+    double least = 0.0;
+    for (int length : {256, 512, 768, 1024, 1536, 2048, 3072, 4096}) {
+        const int64_t workgroups = heads * parts_of(n, length);
+        const double price = codes ? length + (double)n / length * (17.0 + 0.3 * (double)heads)
+                                   : length * (workgroups > 256 && workgroups < 2048 ? 2.0 : 1.0) + (double)n / length * (30.0 + 0.7 * (double)heads);
+        if (keys == 0 || price < least) {
+            keys = length;
+            least = price;
+        }
+    }
+    while (heads * parts_of(n, keys) > kMostPartWorkgroups) keys *= 2;
+    return FewPlan{(int)rows, keys, parts_of(n, keys)};
+}
+// The plan for no more than `there` of n keys, with no more parts than the workspace of n has room for.
+static FewPlan paged_plan_within(int S, int Hq, int Hk, int max_q, int n, int there, bool codes) {
+    const FewPlan given = paged_plan(S, Hq, Hk, max_q, n, codes);
+    if (given.rows == 0 || n <= there) return given;
+    FewPlan plan = paged_plan(S, Hq, Hk, max_q, there, codes);
+    while (plan.parts > given.parts) {
+        plan.part_keys *= 2;
+        plan.parts = parts_of(there, plan.part_keys);
+    }
+    return plan;
 }
 
 template <class T, int E, int NQB, bool CODES>
@@ -665,12 +699,18 @@ static int32_t launch_paged(PagedParams p, const FewPlan& few, int most_keys, vo
 
 using namespace chipmunk;
 
-// The keys that a plan divides: those that are numbered, in whole tiles.
-static int planned_keys(int max_q, int max_k, int window, int sinks) { return most_numbered(max_q, max_k, window, sinks, kStepKeys); }
+
+// The form that a call takes and, for parts, their keys, for the tests.
+extern "C" int chipmunk_internal_attn_paged_form(int S, int Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal, int window, int sinks, int codes) {
+    const int n = most_numbered(max_q, max_k, window, sinks);
+    const FewPlan few = paged_plan(S, Hq, Hk, max_q, n, codes != 0);
+    return few.rows > 0 ? few.part_keys : packed_form(S, Tq, Hq, Hk, E, std::min(max_q, Tq), n, causal);
+}
 
 extern "C" size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks) {
     if (S <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (E != 64 && E != 128) || max_q <= 0 || max_k <= 0 || window < 0 || sinks < 0) return 0;
-    return few_bytes(few_plan(S, Hq, Hk, max_q, planned_keys(max_q, max_k, window, sinks)), S, Hk, E);
+    const int n = most_numbered(max_q, max_k, window, sinks);
+    return std::max(few_bytes(paged_plan(S, Hq, Hk, max_q, n, false), S, Hk, E), few_bytes(paged_plan(S, Hq, Hk, max_q, n, true), S, Hk, E));
 }
 
 extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
@@ -697,13 +737,13 @@ extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride
         (q_token_stride | out_token_stride) % 8 != 0 || (Hq > 1 && (q_head_stride | out_head_stride) % 8 != 0))
         return CHIPMUNK_ERR_ALIGN;
     const int most_keys = std::min(max_k, table_pages * held.page_size);
-    const int given = planned_keys(max_q, max_k, window, sinks);   // as the workspace was asked for
+    const int given = most_numbered(max_q, max_k, window, sinks);   // as the workspace was asked for
     if (window >= most_keys) window = 0;                  // (which every query sees whole)
     PagedParams p{{q, out, cu_q, q_token_stride, q_head_stride, out_token_stride, out_head_stride, S, Tq, Hq, Hk, Hq / Hk, std::min(max_q, Tq), most_keys, causal != 0, 0, 0, 0, 0,
                    nullptr, sl2},
                   held, table, k_len, table_stride, most_keys, window, window ? sinks : 0, __builtin_ctz((uint32_t)held.page_size), 0};
-    const int planned = planned_keys(max_q, most_keys, window, sinks);
-    const FewPlan few = few_plan_within(S, Hq, Hk, max_q, given, planned);
+    const int planned = most_numbered(max_q, most_keys, window, sinks);
+    const FewPlan few = paged_plan_within(S, Hq, Hk, max_q, given, planned, held.format == CHIPMUNK_DTYPE_E4M3);
     const auto st = static_cast<hipStream_t>(stream);
     auto go = [&](auto type, auto width) {
         typedef decltype(type) T;
