@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
 // two tiles of 32.  Elements go from the pages to LDS by asynchronous loads, double buffered by step; codes are in registers a step before, and go to LDS
 // as elements while the step before theirs is computed.
 template <class T, int E, int NQB, bool CODES>
-__global__ __launch_bounds__(256, E == 64 && NQB <= 2 ? 3 : 2) void attn_paged_rows_kernel(PagedParams p) {
+__global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(PagedParams p) {
     typedef typename T::x8 x8;
     constexpr int NWAVES = 4, ROWS = 16 * NQB * NWAVES;
     constexpr int ROWB = E * 2;                           // bytes per K/V row of a tile
@@ -607,39 +607,80 @@ static int most_numbered(int max_q, int max_k, int window, int sinks) {
     return (int)std::min<int64_t>(most, max_k);
 }
 
-// Up to 32 rows of a key head: parts of so many of n numbered keys, as few_plan has them, or whole sequences (rows 0).  A part of codes costs half as
-// many keys' time to begin and end, and three workgroups stand on a CU; of elements two, and more than one and less than eight workgroups to a
-// CU leave some without work.  Measured on 4009 batches of 1 to 128 sequences, 300 to 40 000 keys, ragged and not: the length taken
-// takes 1.03 times the quickest's time in the mean (as few_plan has it 1.06 of codes, 1.04 of elements).
-static FewPlan paged_plan(int S, int Hq, int Hk, int max_q, int n, bool codes) {
+// Up to 1024 rows of a key head may walk their n numbered keys in parts, whose length goes by its price.  A part of codes takes half the time to begin and end
+// that one of elements does.  Measured on 4009 batches of up to 32 rows (1 to 128 sequences of 300 to 40 000 keys, ragged and not) and 5294 of more (1 to 8
+// sequences, with windows and without): parts or whole, and their length, take 1.03 times the quickest's time in the mean in either, of
+// codes and of elements (by the rules of packed attention 1.06 and 1.04; 1.07 and 1.05; 6.5 at most).
+struct PartsPlan {
+    FewPlan few;              // rows 0: none
+    double price;             // us; of more than 32 rows
+};
+struct PartsPrice {
+    float start, keys, join, join_block, share;   // of a launch; 64 keys of 64 rows; a part's joining, for each block of 64 rows; workgroups that have work
+};
+constexpr PartsPrice kPartsPrices[2][2] = {{{6.f, 0.5f, 0.073f, 0.002f, 0.71f}, {14.f, 0.66f, 0.38f, 0.0015f, 0.89f}},   // elements: E = 64, 128
+                                           {{6.5f, 0.62f, 0.17f, 0.0008f, 0.56f}, {6.8f, 0.9f, 0.17f, 0.002f, 1.1f}}};   // codes
+constexpr int64_t kMostPartRows = 1 << 19;    // rows of all parts in the workspace, of more than 32 rows (272 MB at E = 128)
+static PartsPlan parts_plan(int S, int Hq, int Hk, int E, int max_q, int n, bool codes) {
+    const PartsPlan none{FewPlan{0, 0, 0}, HUGE_VAL};
     const int64_t rows = (int64_t)max_q * (Hq / Hk), heads = (int64_t)S * Hk;
-    if (rows > 32 || heads > kMostPartWorkgroups / 2) return few_plan(S, Hq, Hk, max_q, n);
-    if (n <= (codes ? std::min<int64_t>(700 + 4 * heads, 3000) : std::min<int64_t>(1000 + 15 * heads, 3000))) return FewPlan{0, 0, 0};
-    int keys = 0;
-    double least = 0.0;
+    if (rows > 1024 || heads > kMostPartWorkgroups / 2) return none;
+    const bool few = rows <= 32;
+    if (few && n <= (codes ? std::min<int64_t>(700 + 4 * heads, 3000) : std::min<int64_t>(1000 + 15 * heads, 3000))) return none;
+    const int64_t blocks = heads * ((rows + 63) / 64);
+    const PartsPrice& f = kPartsPrices[codes][E == 128];
+    PartsPlan best = none;
     for (int length : {256, 512, 768, 1024, 1536, 2048, 3072, 4096}) {
-        const int64_t workgroups = heads * parts_of(n, length);
-        const double price = codes ? length + (double)n / length * (17.0 + 0.3 * (double)heads)
-                                   : length * (workgroups > 256 && workgroups < 2048 ? 2.0 : 1.0) + (double)n / length * (30.0 + 0.7 * (double)heads);
-        if (keys == 0 || price < least) {
-            keys = length;
-            least = price;
-        }
+        const int64_t workgroups = blocks * parts_of(n, length);
+        const double parts = (double)n / length;
+        double price;
+        if (few) price = codes ? length + parts * (17.0 + 0.3 * (double)heads)
+                               : length * (workgroups > 256 && workgroups < 2048 ? 2.0 : 1.0) + parts * (30.0 + 0.7 * (double)heads);
+        else price = f.start + length / 64.0 * f.keys * std::max(1.0, (double)workgroups * f.share / 256) + parts * (f.join + f.join_block * (double)blocks);
+        if (!few && (length < 512 || heads * parts_of(n, length) * rows > kMostPartRows)) continue;
+        if (best.few.rows == 0 || price < best.price) best = PartsPlan{FewPlan{(int)rows, length, parts_of(n, length)}, price};
     }
-    while (heads * parts_of(n, keys) > kMostPartWorkgroups) keys *= 2;
-    return FewPlan{(int)rows, keys, parts_of(n, keys)};
+    // (a limit may be far above the lengths: the parts grow with it)
+    while (best.few.rows > 0 && blocks * best.few.parts > kMostPartWorkgroups) {
+        best.few.part_keys *= 2;
+        best.few.parts = parts_of(n, best.few.part_keys);
+    }
+    return best;
 }
-// The plan for no more than `there` of n keys, with no more parts than the workspace of n has room for.
-static FewPlan paged_plan_within(int S, int Hq, int Hk, int max_q, int n, int there, bool codes) {
-    const FewPlan given = paged_plan(S, Hq, Hk, max_q, n, codes);
-    if (given.rows == 0 || n <= there) return given;
-    FewPlan plan = paged_plan(S, Hq, Hk, max_q, there, codes);
-    while (plan.parts > given.parts) {
-        plan.part_keys *= 2;
-        plan.parts = parts_of(there, plan.part_keys);
+// The plan for `there` of n keys, with no more parts than the workspace of n has room for.
+static PartsPlan parts_plan_within(int S, int Hq, int Hk, int E, int max_q, int n, int there, bool codes) {
+    const PartsPlan given = parts_plan(S, Hq, Hk, E, max_q, n, codes);
+    if (given.few.rows == 0 || n <= there) return given;
+    PartsPlan plan = parts_plan(S, Hq, Hk, E, max_q, there, codes);
+    while (plan.few.parts > given.few.parts) {
+        plan.few.part_keys *= 2;
+        plan.few.parts = parts_of(there, plan.few.part_keys);
     }
     return plan;
 }
+
+// Whole sequences, as packed_price has it, fitted to the 5294 batches.  (192 rows were the quickest in 22 of them, and twice as slow as 128 of codes at
+// E = 128, whose registers they pass; there are none here.)
+constexpr int kPagedForms = kRows192;
+constexpr PackedPrice kPagedPrices[2][2][kPagedForms] = {
+    {{{16, 3.7f, 0.17f, 0.58f}, {32, 6.1f, 0.25f, 0.29f}, {64, 3.1f, 0.9f, 0.32f}, {128, 5.9f, 1.31f, 0.246f}},
+     {{16, 5.f, 0.165f, 1.72f}, {32, 8.f, 0.45f, 0.58f}, {64, 5.1f, 0.85f, 0.64f}, {128, 7.f, 1.32f, 0.18f}}},
+    {{{16, 3.5f, 0.31f, 0.745f}, {32, 6.1f, 0.33f, 0.37f}, {64, 3.1f, 1.01f, 0.45f}, {128, 4.8f, 1.04f, 0.24f}},
+     {{16, 2.7f, 0.36f, 1.78f}, {32, 6.9f, 0.39f, 0.72f}, {64, 5.9f, 0.84f, 0.61f}, {128, 5.85f, 1.18f, 0.38f}}}};
+constexpr float kPagedLast[2][2] = {{0.25f, 0.53f}, {0.235f, 0.56f}};
+struct WholePlan {
+    PackedForm form;
+    double price;             // HUGE_VAL: no form's launch covers it
+};
+static WholePlan whole_plan(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int n, int causal, bool codes) {
+    WholePlan best{kKeys16, HUGE_VAL};
+    for (int f = 0; f < kPagedForms; f++) {
+        const double price = form_price((PackedForm)f, kPagedPrices[codes][E == 128][f], kPagedLast[codes][E == 128], S, Tq, Hq, Hk, max_q, n, causal);
+        if (price < best.price) best = WholePlan{(PackedForm)f, price};
+    }
+    return best;
+}
+static bool in_parts(const PartsPlan& parts, const WholePlan& whole) { return parts.few.rows > 0 && (parts.few.rows <= 32 || parts.price < whole.price); }
 
 template <class T, int E, int NQB, bool CODES>
 static int32_t launch_paged_rows(PagedParams p, hipStream_t stream) {
@@ -668,8 +709,10 @@ static int32_t launch_paged_few(PagedParams p, hipStream_t stream) {
 }
 
 template <class T, int E, bool CODES>
-static int32_t launch_paged(PagedParams p, const FewPlan& few, int most_keys, void* ws, size_t ws_bytes, hipStream_t stream) {
-    if (few.rows > 0) {
+static int32_t launch_paged(PagedParams p, const PartsPlan& parts, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const WholePlan whole = whole_plan(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, n, p.causal, CODES);
+    if (in_parts(parts, whole)) {
+        const FewPlan& few = parts.few;
         if (few_bytes(few, p.S, p.Hk, E) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
         p.few_rows = few.rows;
         p.part_keys = few.part_keys;
@@ -679,19 +722,17 @@ static int32_t launch_paged(PagedParams p, const FewPlan& few, int most_keys, vo
                : few.rows <= 32 ? launch_paged_few<T, E, 2, CODES>(p, stream)
                                 : launch_paged_few<T, E, 4, CODES>(p, stream);
     }
-    const PackedForm form = packed_form(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, most_keys, p.causal);
-    if (packed_price(form, p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, most_keys, p.causal) == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;   // no form's launch covers it
-    if (form <= kKeys32) {
+    if (whole.price == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;
+    if (whole.form <= kKeys32) {
         p.few_rows = p.max_q * p.G;
         p.part_keys = INT32_MAX;
         p.parts = 1;
     }
-    switch (form) {
+    switch (whole.form) {
         case kKeys16: return launch_paged_few<T, E, 1, CODES>(p, stream);
         case kKeys32: return launch_paged_few<T, E, 2, CODES>(p, stream);
         case kRows64: return launch_paged_rows<T, E, 1, CODES>(p, stream);
-        case kRows128: return launch_paged_rows<T, E, 2, CODES>(p, stream);
-        default: return launch_paged_rows<T, E, 3, CODES>(p, stream);
+        default: return launch_paged_rows<T, E, 2, CODES>(p, stream);
     }
 }
 
@@ -703,14 +744,15 @@ using namespace chipmunk;
 // The form that a call takes and, for parts, their keys, for the tests.
 extern "C" int chipmunk_internal_attn_paged_form(int S, int Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal, int window, int sinks, int codes) {
     const int n = most_numbered(max_q, max_k, window, sinks);
-    const FewPlan few = paged_plan(S, Hq, Hk, max_q, n, codes != 0);
-    return few.rows > 0 ? few.part_keys : packed_form(S, Tq, Hq, Hk, E, std::min(max_q, Tq), n, causal);
+    const PartsPlan parts = parts_plan(S, Hq, Hk, E, max_q, n, codes != 0);
+    const WholePlan whole = whole_plan(S, Tq, Hq, Hk, E, std::min(max_q, Tq), n, causal, codes != 0);
+    return in_parts(parts, whole) ? parts.few.part_keys : whole.form;
 }
 
 extern "C" size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks) {
     if (S <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (E != 64 && E != 128) || max_q <= 0 || max_k <= 0 || window < 0 || sinks < 0) return 0;
-    const int n = most_numbered(max_q, max_k, window, sinks);
-    return std::max(few_bytes(paged_plan(S, Hq, Hk, max_q, n, false), S, Hk, E), few_bytes(paged_plan(S, Hq, Hk, max_q, n, true), S, Hk, E));
+    const int n = most_numbered(max_q, max_k, window, sinks);   // (of either format)
+    return std::max(few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, false).few, S, Hk, E), few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, true).few, S, Hk, E));
 }
 
 extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
@@ -743,12 +785,12 @@ extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride
                    nullptr, sl2},
                   held, table, k_len, table_stride, most_keys, window, window ? sinks : 0, __builtin_ctz((uint32_t)held.page_size), 0};
     const int planned = most_numbered(max_q, most_keys, window, sinks);
-    const FewPlan few = paged_plan_within(S, Hq, Hk, max_q, given, planned, held.format == CHIPMUNK_DTYPE_E4M3);
+    const PartsPlan parts = parts_plan_within(S, Hq, Hk, E, max_q, given, planned, held.format == CHIPMUNK_DTYPE_E4M3);
     const auto st = static_cast<hipStream_t>(stream);
     auto go = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
-        return held.format == CHIPMUNK_DTYPE_E4M3 ? launch_paged<T, W, true>(p, few, planned, ws, ws_bytes, st) : launch_paged<T, W, false>(p, few, planned, ws, ws_bytes, st);
+        return held.format == CHIPMUNK_DTYPE_E4M3 ? launch_paged<T, W, true>(p, parts, planned, ws, ws_bytes, st) : launch_paged<T, W, false>(p, parts, planned, ws, ws_bytes, st);
     };
     typedef std::integral_constant<int, 64> Narrow;
     typedef std::integral_constant<int, 128> Wide;

@@ -474,8 +474,8 @@ constexpr PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.8f, 0.17f, 0.81f
                                                            {{16, 5.5f, 0.165f, 1.78f}, {32, 8.3f, 0.43f, 0.70f}, {64, 5.1f, 0.94f, 0.64f}, {128, 5.1f, 1.49f, 0.50f}, {192, 13.8f, 2.34f, 0.41f}}};
 constexpr float kPackedLast[2][2] = {{0.35f, 0.25f}, {0.49f, 0.53f}};   // of E = 64, 128; all keys, causal
 constexpr double kPackedEmpty = 0.0008;               // us
-inline double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
-    const PackedPrice& f = kPackedPrices[E == 128][form];
+// last_share: of the last workgroup
+inline double form_price(PackedForm form, const PackedPrice& f, double last_share, int S, int64_t Tq, int Hq, int Hk, int max_q, int max_k, int causal) {
     const bool grouped = form <= kKeys32;                 // rows of a key head, of all its queries' heads
     const double launched = (grouped ? few_grid(f.rows, S, Hk, (int64_t)max_q * (Hq / Hk), 1) : rows_grid(f.rows, S, Tq, Hq, Hk, max_q)).workgroups;
     if (launched >= kMostWorkgroups) return HUGE_VAL;
@@ -490,8 +490,11 @@ inline double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, i
     };
     add(1, max_q, max_k);
     if (S > 1) add(S - 1, rest, rest * max_k / max_q);
-    const double longest = max_k / 64.0, last = kPackedLast[E == 128][causal != 0] * longest * (f.rows / 64.0) * f.full;
+    const double longest = max_k / 64.0, last = last_share * longest * (f.rows / 64.0) * f.full;
     return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last) + kPackedEmpty * std::max(0.0, launched - workgroups);
+}
+inline double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
+    return form_price(form, kPackedPrices[E == 128][form], kPackedLast[E == 128][causal != 0], S, Tq, Hq, Hk, max_q, max_k, causal);
 }
 inline PackedForm packed_form(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
     PackedForm best = kKeys16;

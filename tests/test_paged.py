@@ -263,26 +263,64 @@ def test_windows(cm, nq, nk, window, sinks):
         Batch(cm, nq, nk, Hq, Hk, E, dtype, fmt, page, seed=max(nk) + i).check(True, None, window, sinks)
 
 
-# one batch for each form: rows of a tile / 64 + 1 or, of a key head's rows, 0 (16) and 1 (32)
-FORMS = [(64, 2, 40, 40, [130, 60, 0, 1]), (64, 3, 40, 40, [1201, 701, 1, 1201, 33, 701, 0, 701, 701]), (64, 4, 64, 8, [8003, 1, 0, 70]), (128, 2, 40, 40, [130, 60, 0, 1]),
-         (128, 3, 40, 40, [301, 1, 301, 301, 301, 0]), (128, 4, 32, 8, [4003, 0, 1, 31])]
+# one batch for each form of whole sequences, of elements and of codes: 0 and 1: 16 and 32 rows of a key head, 2 and 3: 64 and 128 of a head
+FORMS = [(128, 0, 0, 1, 1, [43, 6, 20, 32]), (128, 0, 1, 2, 2, [2761]), (128, 0, 2, 40, 8, [62, 7, 17, 17, 1, 2]), (128, 0, 3, 40, 8, [179, 95, 62, 175, 174, 169]),
+         (128, 1, 0, 1, 1, [101]), (128, 1, 1, 2, 2, [2338]), (128, 1, 2, 40, 8, [127, 2, 122, 10, 85, 23]), (128, 1, 3, 40, 8, [97, 50, 87, 42, 79, 86]),
+         (64, 0, 0, 1, 1, [101]), (64, 0, 1, 8, 8, [1572, 6]), (64, 0, 2, 1, 1, [38, 20, 35, 8]), (64, 0, 3, 32, 8, [1937, 1884]),
+         (64, 1, 0, 1, 1, [101]), (64, 1, 1, 8, 8, [1482, 105, 5, 25]), (64, 1, 2, 1, 1, [30, 7, 6, 14, 29, 15]), (64, 1, 3, 40, 8, [360, 138, 194, 64, 228, 37])]
+# and of more than 32 rows of a key head over keys in parts: E, codes, keys of a part, Hq, Hk, nq, nk
+DIVIDED = [(128, 0, 512, 1, 1, [33], [6276]), (128, 0, 1024, 8, 8, [33, 1, 0, 20, 33, 7], [5404, 5000, 3, 1025, 40, 7]), (128, 1, 512, 1, 1, [35], [2775]), (128, 1, 768, 4, 4, [71, 70, 1, 60], [5156, 4000, 769, 768]),
+           (64, 0, 768, 4, 4, [65, 2, 3, 65], [7586, 7000, 1, 300]), (64, 1, 1024, 4, 4, [130, 9, 1, 2], [8589, 1024, 1025, 3000]), (64, 1, 512, 1, 1, [33], [2378])]
+
+
+def _form(cm, E, Hq, Hk, nq, nk, codes, window=0, sinks=0, causal=1):
+    Tq = len(nq) * max(nq) if nk is not nq else sum(nq)
+    return cm.load().chipmunk_internal_attn_paged_form(len(nq), Tq, Hq, Hk, E, max(nq), max(nk), causal, window, sinks, codes)
+
+
+def test_the_forms_are_what_the_batches_take(cm):
+    for E, codes, form, Hq, Hk, lengths in FORMS:
+        assert _form(cm, E, Hq, Hk, lengths, lengths, codes) == form == _form(cm, E, Hq, Hk, lengths, lengths, codes, 150, 70)
+    for E, codes, keys, Hq, Hk, nq, nk in DIVIDED:
+        assert _form(cm, E, Hq, Hk, nq, nk, codes) == keys and max(nq) * Hq // Hk > 32
 
 
 @gpu
-@pytest.mark.parametrize("E,form,Hq,Hk,lengths", FORMS)
+@pytest.mark.parametrize("E,codes,form,Hq,Hk,lengths", FORMS)
 @pytest.mark.parametrize("window,sinks", [(0, 0), (150, 70)])
-def test_large_batches(cm, E, form, Hq, Hk, lengths, window, sinks):
-    for dtype, fmt in ((torch.bfloat16, E4M3), (torch.float16, torch.float16)):
-        b = Batch(cm, lengths, lengths, Hq, Hk, E, dtype, fmt, 64, seed=form)
-        out = b.run(True, None, window, sinks)
-        assert not bool(out.isnan().any()) and torch.equal(b.run(True, None, window, sinks), out)
+def test_every_form(cm, E, codes, form, Hq, Hk, lengths, window, sinks):
+    for dtype in TYPES:
+        Batch(cm, lengths, lengths, Hq, Hk, E, dtype, E4M3 if codes else dtype, 64, seed=form).check(True, None, window, sinks)
+
+
+@gpu
+@pytest.mark.parametrize("E,codes,keys,Hq,Hk,nq,nk", DIVIDED)
+def test_many_rows_over_divided_keys(cm, E, codes, keys, Hq, Hk, nq, nk):
+    for dtype in TYPES:
+        b = Batch(cm, nq, nk, Hq, Hk, E, dtype, E4M3 if codes else dtype, 32, seed=keys)
+        q = torch.zeros((len(nq) * max(nq), Hq, E), dtype=dtype, device=DEV)      # (the tensor's rows are as many as the limit says)
+        q[:b.q.shape[0]] = b.q
+        b.q = q
+        for window, sinks in ((0, 0), (2000, 40)):
+            b.check(True, None, window, sinks)
+        b.check(False)
+
+
+@gpu
+def test_large_batches(cm):
+    """More workgroups than stand on the card at a time."""
+    lengths = [2003, 1, 1201, 701, 0, 700]
+    for E, dtype, fmt in ((128, torch.bfloat16, E4M3), (64, torch.float16, E4M3), (128, torch.float16, torch.float16), (64, torch.bfloat16, torch.bfloat16)):
+        b = Batch(cm, lengths, lengths, 40, 40, E, dtype, fmt, 64, seed=E)
         at = _starts(lengths)
-        for s, n in enumerate(lengths):
-            k, v = b.held(s)
-            for h in (0, Hq // 2 + 1, Hq - 1):
-                g = h // (Hq // Hk)
-                want, off = reference(b.q[at[s]:at[s] + n, h:h + 1], k[:, g:g + 1], v[:, g:g + 1], True, E ** -0.5, window, sinks)
-                assert bool(((out[at[s]:at[s] + n, h:h + 1].double() - want).abs() <= off).all()), (s, n, h)
+        for window, sinks in ((0, 0), (150, 70)):
+            out = b.run(True, None, window, sinks)
+            assert not bool(out.isnan().any()) and torch.equal(b.run(True, None, window, sinks), out)
+            for s, n in enumerate(lengths):
+                k, v = b.held(s)
+                for h in (0, 21, 39):
+                    want, off = reference(b.q[at[s]:at[s] + n, h:h + 1], k[:, h:h + 1], v[:, h:h + 1], True, E ** -0.5, window, sinks)
+                    assert bool(((out[at[s]:at[s] + n, h:h + 1].double() - want).abs() <= off).all()), (s, n, h)
 
 
 @gpu
