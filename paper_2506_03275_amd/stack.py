@@ -14,15 +14,16 @@ with pre-generated inputs; what carries over to a model is that the index work n
 
 AttentionLayer is attention with its projections and residual, without norms and gates, for sequences packed one behind the other: a
 text encoder over prompts of different lengths, images of different sizes, or single tokens over what their caches hold.
+PagedAttentionLayer is the same with norms of queries and keys, over caches in pages, in 16 or 8 bits, and with a window of keys.
 """
 import math
 
 import torch
 
-from . import (ACT_GELU_TANH, attn_dense, attn_dense_colsum_stale, attn_dense_row_stats,
-               attn_dense_workspace_bytes, attn_packed, attn_packed_workspace_bytes, attn_sparse_delta, linear, mlp_dense,
-               mlp_sparse_delta, mlp_tile_mean_preact, mlp_tile_mean_workspace_bytes, mlp_workspace_bytes, rope,
-               topk_cols)
+from . import (ACT_GELU_TANH, Pages, attn_dense, attn_dense_colsum_stale, attn_dense_row_stats,
+               attn_dense_workspace_bytes, attn_packed, attn_packed_workspace_bytes, attn_paged, attn_paged_workspace_bytes,
+               attn_sparse_delta, cache_write, linear, mlp_dense, mlp_sparse_delta, mlp_tile_mean_preact,
+               mlp_tile_mean_workspace_bytes, mlp_workspace_bytes, norm_rope, rope, topk_cols)
 
 
 def _u8(nbytes, dev):
@@ -182,5 +183,52 @@ class AttentionLayer:
         self.v_cache.index_copy_(0, rows, qkv[:, H + Hk:])
         attn_packed(qkv[:, :H], self.k_cache, self.v_cache, cu_q, self.starts, b["att"], b["max_q"], b["max_k"], self.causal, self.scale,
                     k_len=k_len, ws=b["ws"])
+        linear(b["att"].view(b["att"].shape[0], -1), self.w_out, self.b_out, x, b["out"])
+        return b["out"]
+
+
+def empty_pages(count, page_size, kv_heads, E, dtype, device="cuda"):
+    """Pages for so many times page_size tokens, of bfloat16, float16 or float8_e4m3fn; a page's scales of one head lie side by side."""
+    k, v = (torch.empty((count, page_size, kv_heads, E), dtype=dtype, device=device) for _ in "kv")
+    if dtype is not torch.float8_e4m3fn:
+        return Pages(k, v)
+    scales = (torch.empty((count, kv_heads, page_size), dtype=torch.uint8, device=device).transpose(1, 2) for _ in "kv")
+    return Pages(k, v, *scales)
+
+
+class PagedAttentionLayer:
+    """x + W_out attention(turn(norm(W_qkv x))) over packed sequences, whose keys and values are kept in pages.
+
+    w_qkv, b_qkv, w_out, b_out, freqs, axes, halves: as AttentionLayer takes them; q_norm, k_norm: [E], the weights of the queries' and the
+    keys' norms; pages: Pages (empty_pages), whose heads are the keys'; window, sinks: as attn_paged takes them.
+    """
+
+    def __init__(self, w_qkv, b_qkv, w_out, b_out, heads, q_norm, k_norm, freqs, axes, pages, causal=True, halves=False, window=0, sinks=0, eps=1e-6):
+        self.w_qkv, self.b_qkv, self.w_out, self.b_out, self.freqs, self.axes = w_qkv, b_qkv, w_out, b_out, freqs, axes
+        self.q_norm, self.k_norm, self.eps, self.pages = q_norm, k_norm, eps, pages
+        self.heads, self.kv_heads, self.E = heads, pages.k.shape[2], pages.k.shape[3]
+        self.causal, self.halves, self.window, self.sinks = causal, halves, window, sinks
+        self.scale = 1.0 / math.sqrt(self.E)
+
+    def buffers(self, tokens, sequences, max_q, max_k):
+        """What a step over so many tokens works in: projections, attention and result, and the workspace.  Two steps that may
+        overlap, also as captured graphs, need buffers of their own."""
+        like = dict(dtype=self.w_qkv.dtype, device=self.w_qkv.device)
+        bytes = attn_paged_workspace_bytes(sequences, self.heads, self.kv_heads, self.E, max_q, max_k, self.window, self.sinks)
+        return dict(qkv=torch.empty((tokens, self.heads + 2 * self.kv_heads, self.E), **like), att=torch.empty((tokens, self.heads, self.E), **like),
+                    out=torch.empty((tokens, self.w_out.shape[0]), **like), max_q=max_q, max_k=max_k, ws=_u8(bytes, self.w_qkv.device))
+
+    def step(self, x, pos, cu_q, rows, k_len, table, buffers):
+        """x: [tokens, D], the sequences one behind the other (cu_q int32 [sequences + 1]); pos: int32 [tokens, 3]; rows: int64 [tokens], each
+        token's row of the pages (page * page_size + place), negative: its keys and values are not kept; k_len: int32 [sequences], tokens of
+        each, the new ones among them; table: int32 [sequences, pages], the pages of each.  Tokens behind cu_q's last entry (a padded
+        batch, whose rows are negative) have no influence on the others and results without meaning.  Returns buffers["out"]."""
+        b, H, Hk = buffers, self.heads, self.kv_heads
+        qkv = b["qkv"]
+        linear(x, self.w_qkv, self.b_qkv, None, qkv.view(qkv.shape[0], -1))
+        turned = qkv[:, :H + Hk]
+        norm_rope(turned, self.q_norm, self.k_norm, H, pos, self.freqs, turned, self.axes, self.eps, halves=self.halves)
+        cache_write(qkv[:, H:H + Hk], qkv[:, H + Hk:], rows, self.pages)
+        attn_paged(qkv[:, :H], self.pages, table, cu_q, k_len, b["att"], b["max_q"], b["max_k"], self.causal, self.scale, self.window, self.sinks, ws=b["ws"])
         linear(b["att"].view(b["att"].shape[0], -1), self.w_out, self.b_out, x, b["out"])
         return b["out"]
