@@ -200,6 +200,15 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
     if (start64 >= walk.count && part > 0) return;        // (without any key the first part writes zeros)
     const int start = (int)start64, end = (int)std::min<int64_t>(walk.count, start64 + p.part_keys);
 
+    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
+    const int first = start + w * kTile;
+    auto fill_table = [&](int n) {                        // the wave's tiles from numbered key n on
+        const Place at = place_of_group<E, CODES>(p, walk, s, head, n + (lane >> 1) * TURN + (lane & 1) * kGroup);
+        places[w][lane] = at.rows;
+        if (CODES) scale_places[CODES ? w : 0][lane] = at.scales;
+    };
+    if (first < end) fill_table(first);                   // under way together with the queries
+
     RowState<T, E, NQB> st;
     int limit[NQB], low[NQB];                             // the first key that the lane's row does not see; the first of its window
 #pragma unroll
@@ -238,13 +247,6 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
         const int row = i * RPI + lane / CH;
         from[i] = (uint32_t)row * (uint32_t)(token * 2) + (uint32_t)(((lane % CH) ^ tile_swizzle<E>(row)) * 16);
     }
-    constexpr int TURN = 4 * kTile;                       // keys from one tile of a wave to its next
-    const int first = start + w * kTile;
-    auto fill_table = [&](int n) {                        // the wave's tiles from numbered key n on
-        const Place at = place_of_group<E, CODES>(p, walk, s, head, n + (lane >> 1) * TURN + (lane & 1) * kGroup);
-        places[w][lane] = at.rows;
-        if (CODES) scale_places[CODES ? w : 0][lane] = at.scales;
-    };
     auto group = [&](int n, int u) {                      // group u of the tile from numbered key n on; nothing behind the part's end
         return group_of<CODES>(places[w], scale_places[CODES ? w : 0], ((uint32_t)(n - first) / TURN % (kWave / 2)) * 2 + u, n < end);
     };
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
         asm volatile("" ::: "memory");                    // (a wave's LDS accesses are done in order)
     };
     auto request_k = [&](int n) {
-        if ((uint32_t)(n - first) % (kWave / 2 * TURN) == 0 && n < end) fill_table(n);
+        if ((uint32_t)(n - first) % (kWave / 2 * TURN) == 0 && n > first && n < end) fill_table(n);
         request(p.pages.k, p.pages.k_scales, k_codes, n, lds0);
     };
     auto request_v = [&](int n) { request(p.pages.v, p.pages.v_scales, v_codes, n, lds0 + V_TILE); };
@@ -312,11 +314,15 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
             request_v(n + TURN);
         }
     };
-    wait_all_memory();                                    // the queries
     if (n < end) {
         request_k(n);
         request_v(n);
     }
+    // The queries, in registers now: no wait for them inside the loop
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++)
+#pragma unroll
+        for (int es = 0; es < E / 32; es++) asm volatile("" : "+v"(st.Q[es][qb]));
     const int plain_end = min(min(end, walk.upto), limit_of(p, i0, keys, past) - walk.high);
 #pragma unroll 1
     for (; n + kTile <= plain_end; n += TURN) tile(std::false_type{});
@@ -587,10 +593,9 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
 // Joins the parts of the rows that have more than one: a wave per row.
 template <class T, int E>
 __global__ __launch_bounds__(256) void attn_paged_join_kernel(PagedParams p) {
-    const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= (int64_t)p.S * p.Hk * p.few_rows) return;
-    const int row = (int)(id % p.few_rows), head = (int)(id / p.few_rows % p.Hk), s = (int)(id / p.few_rows / p.Hk);
+    const int lane = threadIdx.x & 63, row = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int s = blockIdx.x / p.Hk, head = blockIdx.x % p.Hk;
+    if (row >= p.few_rows) return;
     const Rows qs = queries_of(p, s);
     if (row >= qs.count * p.G) return;
     const int keys = keys_held(p, s), past = keys - qs.count;
@@ -704,7 +709,7 @@ static int32_t launch_paged_few(PagedParams p, hipStream_t stream) {
     p.tiles = (int)grid.tiles;
     p.block_rows = 16 * NQB;
     kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
-    if (p.parts > 1) attn_paged_join_kernel<T, E><<<(uint32_t)(((int64_t)p.S * p.Hk * p.few_rows + 3) / 4), 256, 0, stream>>>(p);
+    if (p.parts > 1) attn_paged_join_kernel<T, E><<<dim3((uint32_t)(p.S * p.Hk), (uint32_t)(p.few_rows + 3) / 4), 256, 0, stream>>>(p);
     return launch_status();
 }
 

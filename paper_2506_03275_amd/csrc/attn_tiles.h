@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace chipmunk {
 
@@ -331,45 +332,59 @@ __device__ __forceinline__ void store_joined(const AttnParams& p, int s, int hea
     }
 }
 
+// Over the wave's lanes, in every one of them: pairs 1, 2, 4, ... lanes apart.
+template <class Op>
+__device__ __forceinline__ float lanes_all(float x, Op&& op) {
+    auto moved = [&](auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xf, 0xf, false)); };
+    x = op(x, moved(std::integral_constant<int, 0xb1>{}));    // quad_perm 1 0 3 2
+    x = op(x, moved(std::integral_constant<int, 0x4e>{}));    // quad_perm 2 3 0 1
+    x = op(x, moved(std::integral_constant<int, 0x141>{}));   // row_half_mirror: four lanes have the same by now
+    x = op(x, moved(std::integral_constant<int, 0x140>{}));   // row_mirror
+    const uint32_t u = __float_as_uint(x);
+    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    const uint32_t w = __float_as_uint(x);
+    const auto t = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return op(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+
 // Joins the `parts` parts of a row of a key head, one wave's work.
 template <class T, int E>
 __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head, int row, int first_query, int parts, bool sees, int lane) {
     const float* sums = p.partial + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * E;
     const float* stats = p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * 2;
     constexpr int PER = E / 64;                           // columns of a lane
+    constexpr int AHEAD = 8;
     float top = -INFINITY, total = 0.f, o[PER] = {};
+    auto load = [&](int part, float (&v)[PER]) {
+        const float* from = sums + (int64_t)part * p.few_rows * E + lane * PER;
+        if constexpr (PER == 2) {
+            const f32x2 x = *reinterpret_cast<const f32x2*>(from);
+            v[0] = x[0];
+            v[PER - 1] = x[1];
+        } else {
+            v[0] = *from;
+        }
+    };
     for (int part0 = 0; part0 < parts; part0 += 64) {     // 64 parts' references and sums at a time
+        const int here = min(64, parts - part0);
         f32x2 mine = f32x2{-INFINITY, 0.f};
         if (part0 + lane < parts) mine = *reinterpret_cast<const f32x2*>(stats + (int64_t)(part0 + lane) * p.few_rows * 2);
-        float most = mine[0];
+        float v[AHEAD][PER];                              // under way together with those
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-        most = fmaxf(most, top);
+        for (int n = 0; n < AHEAD; n++) load(part0 + min(n, here - 1), v[n]);
+        const float most = fmaxf(lanes_all(mine[0], [](float a, float b) { return fmaxf(a, b); }), top);
         const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - most) * p.sl2);
         const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[0] - most) * p.sl2);
-        float add = mine[1] * weight;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
+        const float add = lanes_all(mine[1] * weight, [](float a, float b) { return a + b; });
         total = total * before + add;
         top = most;
 #pragma unroll
         for (int i = 0; i < PER; i++) o[i] *= before;
-        const int here = min(64, parts - part0);
-        auto load = [&](int n, float (&v)[PER]) {
-            const float* from = sums + (int64_t)(part0 + n) * p.few_rows * E + lane * PER;
-            if constexpr (PER == 2) {
-                const f32x2 x = *reinterpret_cast<const f32x2*>(from);
-                v[0] = x[0];
-                v[PER - 1] = x[1];
-            } else {
-                v[0] = *from;
-            }
-        };
-        constexpr int AHEAD = 8;
         for (int n0 = 0; n0 < here; n0 += AHEAD) {
-            float v[AHEAD][PER];
+            float next[AHEAD][PER];
 #pragma unroll
-            for (int n = 0; n < AHEAD; n++) load(min(n0 + n, here - 1), v[n]);
+            for (int n = 0; n < AHEAD; n++) load(part0 + min(n0 + AHEAD + n, here - 1), next[n]);
 #pragma unroll
             for (int n = 0; n < AHEAD; n++) {
                 const float f = n0 + n < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), min(n0 + n, here - 1))) : 0.f;
@@ -377,6 +392,8 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head,
 #pragma unroll
                     for (int i = 0; i < PER; i++) o[i] += v[n][i] * f;
                 }
+#pragma unroll
+                for (int i = 0; i < PER; i++) v[n][i] = next[n][i];
             }
         }
     }

@@ -107,8 +107,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(CacheParams 
         (at.value ? p.pages.v_scales : p.pages.k_scales)[place_of(p, row, at.head, p.pages.scale_page_stride, p.pages.scale_token_stride, p.pages.scale_head_stride)] = (uint8_t)(k + 127);
 }
 
-// RESULT: one beyond the last-level cache passes it by.
-template <class T, bool CODES, int RESULT>
+template <class T, bool CODES>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheParams p) {
     const CacheItem at = cache_item(p);
     if (at.token >= p.tokens) return;
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(CacheParams p
     }
     uint16_t* to = (at.value ? p.to_v + at.token * p.v_token + at.head * p.v_head : p.to_k + at.token * p.k_token + at.head * p.k_head) + at.chunk * 16;
 #pragma unroll
-    for (int i = 0; i < 2; i++) rope_store<RESULT>(raw_buffer(to, 0), to, to + i * 8, x[i]);
+    for (int i = 0; i < 2; i++) reinterpret_cast<u32x4*>(to)[i] = x[i];   // (past the last-level cache 1.4 GB take 268 us for 254)
 }
 
 // The checks that writing and reading share.
@@ -185,13 +184,8 @@ extern "C" int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_
     if (status != CHIPMUNK_OK) return status;
     const auto s = static_cast<hipStream_t>(stream);
     const uint32_t grid = cache_workgroups(p);
-    auto go = [&](auto result) {
-        constexpr int RESULT = decltype(result)::value;
-        if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_read_kernel<Bf16, false, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
-        else if (dtype == CHIPMUNK_DTYPE_BF16) cache_read_kernel<Bf16, true, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
-        else cache_read_kernel<Fp16, true, RESULT><<<grid, kCacheThreads, 0, s>>>(p);
-    };
-    if ((int64_t)tokens * p.pages.heads * p.pages.E * 4 > kRopeLastLevel) go(std::integral_constant<int, kPastLastLevel>{});
-    else go(std::integral_constant<int, kKept>{});
+    if (pages->format != CHIPMUNK_DTYPE_E4M3) cache_read_kernel<Bf16, false><<<grid, kCacheThreads, 0, s>>>(p);
+    else if (dtype == CHIPMUNK_DTYPE_BF16) cache_read_kernel<Bf16, true><<<grid, kCacheThreads, 0, s>>>(p);
+    else cache_read_kernel<Fp16, true><<<grid, kCacheThreads, 0, s>>>(p);
     return launch_status();
 }

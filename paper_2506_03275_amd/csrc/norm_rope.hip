@@ -148,15 +148,16 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p) {
         const uint16_t* from = p.x + t * p.x_token;
         uint16_t* to = p.out + t * p.out_token;
         float c[Item::NP], s[Item::NP];
-        it.angles(p, t, item, c, s);
         for (int h = first_head; h < last_head; h += kNormAhead * p.side) {
             u32x4 a[kNormAhead], b[kNormAhead];
 #pragma unroll
             for (int n = 0; n < kNormAhead; n++) {
-                const int64_t row = (int64_t)min(h + n * p.side, last_head - 1) * p.x_head;
+                if (h + n * p.side >= last_head) break;
+                const int64_t row = (int64_t)(h + n * p.side) * p.x_head;
                 a[n] = rope_load<SOURCE>(from + row + it.e0);
                 if (HALVES) b[n] = rope_load<SOURCE>(from + row + it.e1);
             }
+            if (h == first_head) it.angles(p, t, item, c, s);   // while the first rows are under way
 #pragma unroll
             for (int n = 0; n < kNormAhead; n++) {
                 const int head = h + n * p.side;
@@ -203,12 +204,12 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_grad_kernel(NormParams
         const uint16_t* grad = p.grad + t * p.grad_token;
         uint16_t* to = p.out + t * p.out_token;
         float c[Item::NP], s[Item::NP];
-        it.angles(p, t, item, c, s);
         for (int h = first_head; h < last_head; h += kNormGradAhead * p.side) {
             u32x4 a[kNormGradAhead], b[kNormGradAhead], ga[kNormGradAhead], gb[kNormGradAhead];
 #pragma unroll
             for (int n = 0; n < kNormGradAhead; n++) {
-                const int head = min(h + n * p.side, last_head - 1);
+                const int head = h + n * p.side;
+                if (head >= last_head) break;
                 const uint16_t* row = from + head * p.x_head;
                 const uint16_t* grad_row = grad + head * p.grad_head;
                 a[n] = rope_load<SOURCE>(row + it.e0);
@@ -218,6 +219,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_grad_kernel(NormParams
                     gb[n] = rope_load<SOURCE>(grad_row + it.e1);
                 }
             }
+            if (h == first_head) it.angles(p, t, item, c, s);
 #pragma unroll
             for (int n = 0; n < kNormGradAhead; n++) {
                 const int head = h + n * p.side;
@@ -295,16 +297,23 @@ constexpr int64_t kNormGradWorkgroups = 2048;
 constexpr int kNormGradMost = 12;    // heads of a thread
 
 // How a launch's threads are laid out: rows of a token side by side; a result in heads of rows gets four tokens' rows in one run (rope.hip).
+constexpr int64_t kNormSmall = 1 << 17;   // threads
+static int lanes_of(int items) {
+    int lanes = 1;
+    while (lanes < items) lanes *= 2;
+    return lanes;
+}
 struct NormGrid {
     int items, lanes, side, per, at_once, parts;
     int64_t groups;          // of tokens
 };
 static NormGrid norm_grid(int tokens, int heads, int E, int64_t pairs, bool halves, bool heads_of_rows, bool grad) {
     NormGrid g;
-    int per = grad ? kNormGradAhead : kNormAhead;
+    // Few rows: a head to a thread (8 tokens x 40 heads 5.1 -> 3.8 us; the gradient, whose workgroups have more to begin and end, loses)
+    const bool small = !grad && (int64_t)tokens * heads * lanes_of(halves ? (int)(pairs / 8 + (E - 2 * pairs) / 8) : E / 8) <= kNormSmall;
+    int per = small ? 1 : grad ? kNormGradAhead : kNormAhead;
     g.items = halves ? (int)(pairs / 8 + (E - 2 * pairs) / 8) : E / 8;
-    g.lanes = 1;
-    while (g.lanes < g.items) g.lanes *= 2;
+    g.lanes = lanes_of(g.items);
     const int slots = kNormThreads / g.lanes;
     g.side = std::min(heads_of_rows ? std::min(4, slots) : slots, (heads + per - 1) / per);
     // The gradient's angles serve more heads of a thread where there are workgroups enough: as many as divide the heads best
