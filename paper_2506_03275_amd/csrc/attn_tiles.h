@@ -5,7 +5,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 namespace chipmunk {
 
@@ -200,23 +199,48 @@ __device__ __forceinline__ void tile_values(RowState<T, E, NQB>& st, const f32x4
 #pragma unroll
     for (int qb = 0; qb < NQB; qb++) st.L[qb] = T::product(ones, pop[qb], st.L[qb]);
     __builtin_amdgcn_sched_group_barrier(0x008, NQB, 0);
+    auto read = [&](int eb) {
+        if (eb >= NEB) return;
+        lo[eb] = lds_read_tr16_at(vaddr[eb] + tile_off);
+        hi[eb] = lds_read_tr16_at(vaddr[eb] + tile_off + 16 * ROWB);
+    };
+    auto operand = [&](int eb) { return __builtin_bit_cast(u32x4, (short8v)__builtin_shufflevector(lo[eb], hi[eb], 0, 1, 2, 3, 4, 5, 6, 7)); };
+    auto weigh = [&](int eb, u32x4 words) {
 #pragma unroll
-    for (int eb = 0; eb < NEB; eb++) {
-        if (eb + AHEAD < NEB) {
-            lo[eb + AHEAD] = lds_read_tr16_at(vaddr[eb + AHEAD] + tile_off);
-            hi[eb + AHEAD] = lds_read_tr16_at(vaddr[eb + AHEAD] + tile_off + 16 * ROWB);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        for (int qb = 0; qb < NQB; qb++) st.O[eb][qb] = T::product(__builtin_bit_cast(x8, words), pop[qb], st.O[eb][qb]);
+    };
+    if constexpr (!HIDDEN) {
+#pragma unroll
+        for (int eb = 0; eb < NEB; eb++) {
+            if (eb + AHEAD < NEB) {
+                read(eb + AHEAD);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            weigh(eb, operand(eb));
+            __builtin_amdgcn_sched_group_barrier(0x008, NQB, 0);
         }
-        x8 vop = __builtin_bit_cast(x8, (short8v)__builtin_shufflevector(lo[eb], hi[eb], 0, 1, 2, 3, 4, 5, 6, 7));
-        if constexpr (HIDDEN) {
-            u32x4 words = __builtin_bit_cast(u32x4, vop);
+    } else {
+        // (looked for first: to take them out of every word would cost three times as much as to find that there is none)
 #pragma unroll
-            for (int i = 0; i < 4; i++) words[i] = finite_elements<T>(words[i], found);
-            vop = __builtin_bit_cast(x8, words);
+        for (int eb = 0; eb < NEB; eb += AHEAD) {
+            u32x4 words[AHEAD];
+            uint32_t tops = 0;
+#pragma unroll
+            for (int n = 0; n < AHEAD; n++) {
+                read(eb + AHEAD + n);
+                words[n] = operand(eb + n);
+#pragma unroll
+                for (int i = 0; i < 4; i++) tops |= not_finite<T>(words[n][i]);
+            }
+            if (__builtin_amdgcn_ballot_w64(tops != 0) != 0) {
+#pragma unroll
+                for (int n = 0; n < AHEAD; n++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) words[n][i] = finite_elements<T>(words[n][i], found);
+            }
+#pragma unroll
+            for (int n = 0; n < AHEAD; n++) weigh(eb + n, words[n]);
         }
-#pragma unroll
-        for (int qb = 0; qb < NQB; qb++) st.O[eb][qb] = T::product(vop, pop[qb], st.O[eb][qb]);
-        __builtin_amdgcn_sched_group_barrier(0x008, NQB, 0);
     }
 }
 
@@ -332,22 +356,6 @@ __device__ __forceinline__ void store_joined(const AttnParams& p, int s, int hea
     }
 }
 
-// Over the wave's lanes, in every one of them: pairs 1, 2, 4, ... lanes apart.
-template <class Op>
-__device__ __forceinline__ float lanes_all(float x, Op&& op) {
-    auto moved = [&](auto control) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xf, 0xf, false)); };
-    x = op(x, moved(std::integral_constant<int, 0xb1>{}));    // quad_perm 1 0 3 2
-    x = op(x, moved(std::integral_constant<int, 0x4e>{}));    // quad_perm 2 3 0 1
-    x = op(x, moved(std::integral_constant<int, 0x141>{}));   // row_half_mirror: four lanes have the same by now
-    x = op(x, moved(std::integral_constant<int, 0x140>{}));   // row_mirror
-    const uint32_t u = __float_as_uint(x);
-    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    x = op(__uint_as_float(s[0]), __uint_as_float(s[1]));
-    const uint32_t w = __float_as_uint(x);
-    const auto t = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return op(__uint_as_float(t[0]), __uint_as_float(t[1]));
-}
-
 // Joins the `parts` parts of a row of a key head, one wave's work.
 template <class T, int E>
 __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head, int row, int first_query, int parts, bool sees, int lane) {
@@ -373,10 +381,15 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head,
         float v[AHEAD][PER];                              // under way together with those
 #pragma unroll
         for (int n = 0; n < AHEAD; n++) load(part0 + min(n, here - 1), v[n]);
-        const float most = fmaxf(lanes_all(mine[0], [](float a, float b) { return fmaxf(a, b); }), top);
+        float most = mine[0];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        most = fmaxf(most, top);
         const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - most) * p.sl2);
         const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[0] - most) * p.sl2);
-        const float add = lanes_all(mine[1] * weight, [](float a, float b) { return a + b; });
+        float add = mine[1] * weight;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
         total = total * before + add;
         top = most;
 #pragma unroll
