@@ -205,6 +205,17 @@ def test_rows_of_zeros_and_of_extremes(cm, halves):
 
 
 @gpu
+def test_one_weight_alone(cm):
+    """Where no head has a weight there need not be one."""
+    x, w, other, pos, freqs, rows, r = _inputs(cm, 20, 3, 64, (32, 0, 0), torch.bfloat16, 2)
+    a, b = rows(), rows()
+    cm.norm_rope(x, w, None, 3, pos, freqs, a, (32, 0, 0))
+    cm.norm_rope(x, None, w, 0, pos, freqs, b, (32, 0, 0))
+    want, off = norm_rope_reference(x, w, other, 3, pos, freqs, (32, 0, 0), 1e-6, False)
+    assert torch.equal(a, b) and bool(((a.double() - want).abs() <= off).all())
+
+
+@gpu
 def test_what_lies_between_the_rows_stays(cm):
     x, wq, wk, pos, freqs, _, r = _inputs(cm, 50, 6, 128, (64, 0, 0), torch.float16, 1, "projection")
     held = torch.full((50, 10, 136), 7.0, dtype=torch.float16, device=DEV)

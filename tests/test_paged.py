@@ -484,6 +484,90 @@ def test_on_another_stream_and_in_graphs(cm):
 
 
 @gpu
+@pytest.mark.parametrize("fmt", ["elements", "codes"])
+@pytest.mark.parametrize("E,nq,nk,Hq,Hk", [(64, [70], [70], 2, 1), (64, [1], [9001], 8, 1), (128, [100], [7001], 8, 1), (128, [300], [300], 40, 8)])
+def test_the_largest_and_smallest_scales(cm, fmt, E, nq, nk, Hq, Hk):
+    """The largest score alone, but for rows whose two largest are closer than what 32 bits tell apart (2^-24 of sums of 128 products); or all keys alike."""
+    b = Batch(cm, nq, nk, Hq, Hk, E, torch.bfloat16, E4M3 if fmt == "codes" else torch.bfloat16, 32, seed=3)
+    out = b.run(False, 2.0 ** 127)
+    k, v = b.held(0)
+    for h in range(0, Hq, 7):
+        two = (b.q[:, h].double() @ k[:, h // (Hq // Hk)].double().t()).topk(2, -1)
+        clear = two.values[:, 0] - two.values[:, 1] > 1e-3
+        assert torch.equal(out[clear, h], v[two.indices[clear, 0], h // (Hq // Hk)]) and bool(clear.any())
+    b.check(False, 2.0 ** -140)
+
+
+@gpu
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 70)])
+def test_minus_infinite_scores(cm, window, sinks):
+    """A key whose score is minus infinity has no weight, also where it stands in front of all others, and where the window begins."""
+    b = Batch(cm, [70, 1], [170, 300], 2, 1, 64, torch.bfloat16, torch.bfloat16, 16, seed=9)
+    b.q.abs_().clamp_(min=0.1)
+    at = _starts(b.nq)
+    for s, n in ((0, 20), (1, 200)):
+        kv = b.held(s)
+        kv[0, :n, :, 3] = -math.inf
+        cm.cache_write(kv[0], kv[1], b.rows[s], b.pages)
+    out = b.run(True, 0.1, window, sinks)
+    for s, n in ((0, 20), (1, 200)):
+        k, v = b.held(s)
+        k[:n, :, 3] = 0                                             # (the same without those keys, which are hidden below)
+        q = b.q[at[s]:at[s + 1]]
+        j, place = torch.arange(b.nk[s], device=DEV), torch.arange(b.nq[s], device=DEV)[:, None] + b.nk[s] - b.nq[s]
+        seen = (j <= place) & (j >= n) & ((j > place - window) | (j < sinks) if window else True)
+        for h in range(2):
+            sc = (q[:, h].double() @ k[:, 0].double().t() * 0.1).masked_fill(~seen, -math.inf)
+            w = torch.softmax(sc, 1)
+            want, size = w @ v[:, 0].double(), w @ v[:, 0].double().abs()
+            off = 2.0 ** -8 * (size + 2 * want.abs()) * 1.02 + 1e-4 * size      # (32-bit scores of 64 products: below 1e-4 here)
+            assert bool(((out[at[s]:at[s + 1], h].double() - want).abs() <= off).all())
+
+
+@gpu
+def test_heads_of_rows_and_other_strides(cm):
+    """[heads, rows, E] and rows inside wider ones, and an output with gaps that stay; a table with columns behind it."""
+    for nq, nk in (([130, 40], [130, 40]), ([1, 3], [300, 77])):
+        b = Batch(cm, nq, nk, 4, 2, 128, torch.bfloat16, E4M3, 16, seed=2)
+        want, q = b.run(), b.q
+        b.q = q.transpose(0, 1).contiguous().transpose(0, 1)
+        assert torch.equal(b.run(out=torch.empty_like(b.q)), want)
+        wide = torch.full((q.shape[0], 6, 136), 3.0, dtype=q.dtype, device=DEV)
+        b.run(out=wide[:, 1:5, :128])
+        assert torch.equal(wide[:, 1:5, :128], want) and bool((wide[:, [0, 5]] == 3).all()) and bool((wide[..., 128:] == 3).all())
+        table = torch.full((2, 100), 2 ** 30, dtype=torch.int32, device=DEV)
+        table[:, 7:7 + b.table.shape[1]] = b.table
+        b.table = table[:, 7:7 + b.table.shape[1]]
+        assert torch.equal(b.run(), want)
+
+
+@gpu
+def test_scales_of_other_writers(cm):
+    """Every scale byte with every code: rows come back as the formula has it, 255 as NaN, rounded to the elements' type."""
+    pages = make_pages(cm, 16, 16, 4, 64, E4M3)
+    pages.k.view(torch.uint8).copy_(torch.arange(256, dtype=torch.uint8, device=DEV).view(4, 64).expand(16, 16, 4, 64))
+    pages.k_scales.copy_(torch.arange(256, dtype=torch.uint8, device=DEV).view(16, 16, 1).expand(16, 16, 4))
+    for dtype in TYPES:
+        out = torch.zeros((2, 256, 4, 64), dtype=dtype, device=DEV)
+        cm.cache_read(pages, torch.arange(256, device=DEV), out[0], out[1])
+        codes, _, scales, _ = _flat(pages)
+        want = of_codes(codes, scales, torch.float32).to(dtype)      # (2^128 is infinite in 32 bits: of byte 255)
+        got, want = out[0][:255], want[:255]
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(nan=7.0), want.nan_to_num(nan=7.0)) and bool(out[0][255].isnan().all())
+
+
+def test_the_workspace_of_any_limit_is_bounded(cm):
+    """Up to the largest limits, and as many parts as the limits' plan has; without it the call is refused before anything is launched."""
+    of, most = cm.attn_paged_workspace_bytes, 2 ** 31 - 1
+    for S, Hq, Hk, max_q in ((1, 8, 8, 1), (32, 32, 8, 1), (1, 64, 1, 16), (512, 32, 8, 1), (4096, 32, 8, 1), (2, 8, 8, 1024), (65536, 8, 8, 5), (most, most, most, 1)):
+        for max_k in (300, 5001, 131072, 2 ** 24, most):
+            for window, sinks in ((0, 0), (1, 0), (4096, 4), (most, most)):
+                assert 0 <= of(S, Hq, Hk, 128, max_q, max_k, window, sinks) <= 2 ** 17 * 64 * 130 * 4
+    assert of(32, 32, 8, 128, 1, most) >= of(32, 32, 8, 128, 1, 131072) > of(32, 32, 8, 128, 1, 131072, 4096, 4) > 0
+    assert of(1, 8, 8, 128, most, most) == 0
+
+
+@gpu
 def test_a_batch_of_none(cm):
     b = Batch(cm, [0, 0], [50, 0], 4, 2, 64, torch.bfloat16, E4M3, 16)
     out = b.run()
