@@ -222,24 +222,17 @@ __device__ __forceinline__ void tile_values(RowState<T, E, NQB>& st, const f32x4
     } else {
         // (looked for first: to take them out of every word would cost three times as much as to find that there is none)
 #pragma unroll
-        for (int eb = 0; eb < NEB; eb += AHEAD) {
-            u32x4 words[AHEAD];
+        for (int eb = 0; eb < NEB; eb++) {
+            read(eb + AHEAD);
+            u32x4 words = operand(eb);
             uint32_t tops = 0;
 #pragma unroll
-            for (int n = 0; n < AHEAD; n++) {
-                read(eb + AHEAD + n);
-                words[n] = operand(eb + n);
-#pragma unroll
-                for (int i = 0; i < 4; i++) tops |= not_finite<T>(words[n][i]);
-            }
+            for (int i = 0; i < 4; i++) tops |= not_finite<T>(words[i]);
             if (__builtin_amdgcn_ballot_w64(tops != 0) != 0) {
 #pragma unroll
-                for (int n = 0; n < AHEAD; n++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) words[n][i] = finite_elements<T>(words[n][i], found);
+                for (int i = 0; i < 4; i++) words[i] = finite_elements<T>(words[i], found);
             }
-#pragma unroll
-            for (int n = 0; n < AHEAD; n++) weigh(eb + n, words[n]);
+            weigh(eb, words);
         }
     }
 }
