@@ -340,9 +340,15 @@ __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void
     });
 }
 
+// Of rows in parts: the workspace's row of query i of sequence s and a head, [parts][Hq][S][max_q] rows of E sums, then as many references and sums.
+__device__ __forceinline__ int64_t partial_row(const PagedParams& p, int part, int head, int s, int i) { return (((int64_t)part * p.Hq + head) * p.S + s) * p.max_q + i; }
+template <int E>
+__device__ __forceinline__ float* partial_stats(const PagedParams& p) { return p.partial + (int64_t)p.parts * p.Hq * p.S * p.max_q * E; }
+
 // Rows, as attn_packed_rows_kernel: a workgroup of four waves owns 64 NQB consecutive queries of one sequence and head and walks its numbered keys in steps of
 // two tiles of 32.  Elements go from the pages to LDS by asynchronous loads, double buffered by step; codes are in registers a step before, and go to LDS
-// as elements while the step before theirs is computed.
+// as elements while the step before theirs is computed.  Of few rows over many keys a workgroup walks part_keys of them (gridDim.y parts), and
+// attn_paged_join_rows_kernel joins the parts.
 template <class T, int E, int NQB, bool CODES>
 __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(PagedParams p) {
     typedef typename T::x8 x8;
@@ -370,6 +376,10 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     if (rows <= 0) return;
     const int keys = keys_held(p, s), past = keys - qs.count;
     const Walk walk = walk_of<kStepKeys>(p, row0, row0 + rows - 1, keys, past);
+    const int64_t begin64 = (int64_t)blockIdx.y * p.part_keys;
+    if (begin64 >= walk.count && blockIdx.y > 0) return;  // (without any key the first part writes zeros)
+    // The part's keys are numbered from 0 anew.
+    const int begin = (int)begin64, count = (int)std::min<int64_t>(walk.count - begin, p.part_keys);
     const uint16_t* qh = p.q + head * p.q_head + (int64_t)(qs.first + row0) * p.q_token;
     uint16_t* oh = p.out + head * p.out_head + (int64_t)(qs.first + row0) * p.out_token;
     const int kv_head = head / p.G;
@@ -396,7 +406,7 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     const int first_row = row0 + wave_row, last_row = first_row + max(wave_rows, 1) - 1;
     const int seen = wave_rows <= 0 ? 0 : limit_of(p, last_row, keys, past), low_of_any = low_of(p, first_row, past);
     const int seen_by_all = wave_rows <= 0 ? 0 : limit_of(p, first_row, keys, past), low_of_all = low_of(p, last_row, past);
-    const int plain_end = min(walk.upto, seen_by_all - walk.high);
+    const int plain_end = min(count, min(walk.upto, seen_by_all - walk.high) - begin);
     const float slack = kSlack / p.sl2;
 
     const int koff = l16 * ROWB + ((g ^ tile_swizzle<E>(l16)) * 16);
@@ -427,11 +437,11 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     Group at[NG];                                         // of the step that is requested next
     auto next_step = [&](int n) {
 #pragma unroll
-        for (int i = 0; i < NG; i++) at[i] = group_of<CODES>(places, scale_places, ((uint32_t)n / kGroup + group_at(i)) % (2 * kTableGroups), n < walk.count);
+        for (int i = 0; i < NG; i++) at[i] = group_of<CODES>(places, scale_places, ((uint32_t)n / kGroup + group_at(i)) % (2 * kTableGroups), n < count);
     };
     auto fill_table = [&](int n) {                        // the part of the keys from n on
         const int i = (uint32_t)n / kGroup % (2 * kTableGroups) + tid;
-        const Place to = place_of_group<E, CODES>(p, walk, s, kv_head, n + tid * kGroup);
+        const Place to = place_of_group<E, CODES>(p, walk, s, kv_head, begin + n + tid * kGroup);
         places[i] = to.rows;
         if (CODES) scale_places[CODES ? i : 0] = to.scales;
     };
@@ -474,9 +484,9 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     typedef std::integral_constant<int, 0> Even;
     typedef std::integral_constant<int, 1> Odd;
 
-    if (walk.count > 0) {
+    if (count > 0) {
         fill_table(0);
-        if (walk.count > kTableKeys) fill_table(kTableKeys);
+        if (count > kTableKeys) fill_table(kTableKeys);
         wait_all_memory();                                // no wait for the queries inside the loop
         __syncthreads();
         next_step(0);
@@ -498,7 +508,7 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     auto arrived = [&](auto set_c, int half, int n) {
         if constexpr (CODES) lds_accesses_then_barrier();  // the codes stay under way
         else wait_all_memory(), __syncthreads();          // this step's tiles have landed for every wave; the other half is free
-        if ((uint32_t)n % kTableKeys == 0 && n > 0 && n + kTableKeys < walk.count) fill_table(n + kTableKeys);   // (many barriers before its first use)
+        if ((uint32_t)n % kTableKeys == 0 && n > 0 && n + kTableKeys < count) fill_table(n + kTableKeys);   // (many barriers before its first use)
         if constexpr (CODES) {
             put_codes(set_c, half ^ 1);
             next_step(n + (SETS + 1) * kStepKeys);
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
 #pragma unroll
             for (int j = 0; j < E / 16; j++) request(half ^ 1, j);
         }
-        const int key = walk.key(n);
+        const int key = walk.key(begin + n);
         if (nothing_seen(key)) return;
 #pragma unroll
         for (int t = 0; t < kStepTiles; t++) {
@@ -556,10 +566,10 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     const int first_hidden = n;
     if constexpr (CODES) {
 #pragma unroll 1
-        while (n < walk.count) {
+        while (n < count) {
             hidden_step(Odd{}, 0, n, 0);
             n += kStepKeys;
-            if (n >= walk.count) break;
+            if (n >= count) break;
             hidden_step(Even{}, 1, n, kStepTiles * STAGE);
             n += kStepKeys;
         }
@@ -573,7 +583,7 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
         int half = n / kStepKeys & 1;
         move(half * kStepTiles * STAGE);
 #pragma unroll 1
-        for (; n < walk.count; n += kStepKeys, half ^= 1) {
+        for (; n < count; n += kStepKeys, half ^= 1) {
             hidden_step(Even{}, half, n, 0);
             move(half ? -kStepTiles * STAGE : kStepTiles * STAGE);
         }
@@ -583,11 +593,23 @@ __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(P
     // Infinite and NaN values among the steps with hidden keys go to the queries that see them.
     if (__builtin_amdgcn_ballot_w64(found != 0) != 0)
 #pragma unroll 1
-        for (int at = first_hidden; at < walk.count; at += kTile) {
-            const int key = walk.key(at);
+        for (int at = first_hidden; at < count; at += kTile) {
+            const int key = walk.key(begin + at);
             if (!nothing_seen(key / kStepKeys * kStepKeys)) add_special_values<T, E, NQB, CODES>(st, p, s, kv_head, key, walk.end, walk.sinks, limit, low, g);
         }
-    store_rows<T, E, NQB>(st, limit, oh, p.out_token, w * NQB * 16, rows, g, l16);
+    if (walk.count <= p.part_keys) {
+        store_rows<T, E, NQB>(st, limit, oh, p.out_token, w * NQB * 16, rows, g, l16);
+        return;
+    }
+#pragma unroll
+    for (int qb = 0; qb < NQB; qb++) {
+        const int row = (w * NQB + qb) * 16 + l16;
+        if (row >= rows) continue;
+        const int64_t to = partial_row(p, blockIdx.y, head, s, row0 + row);
+#pragma unroll
+        for (int eb = 0; eb < E / 16; eb++) *reinterpret_cast<f32x4*>(p.partial + to * E + eb * 16 + 4 * g) = st.O[eb][qb];
+        if (g == 0) *reinterpret_cast<f32x2*>(partial_stats<E>(p) + to * 2) = f32x2{st.L[qb][0] == 0.f ? -INFINITY : -st.negm[qb][0], st.L[qb][0]};
+    }
 }
 
 // Joins the parts of the rows that have more than one: a wave per row.
@@ -605,10 +627,26 @@ __global__ __launch_bounds__(256) void attn_paged_join_kernel(PagedParams p) {
     join_parts<T, E>(p, s, head, row, qs.first, min((walk.count - 1) / p.part_keys + 1, p.parts), limit_of(p, row / p.G, keys, past) > 0, lane);
 }
 
+// The same of the rows kernel's parts: a wave per query and head.  block_rows: the rows that walked together.
+template <class T, int E>
+__global__ __launch_bounds__(256) void attn_paged_join_rows_kernel(PagedParams p) {
+    const int lane = threadIdx.x & 63, id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
+    const int i = id % p.max_q, s = id / p.max_q;
+    if (s >= p.S) return;
+    const Rows qs = queries_of(p, s);
+    if (i >= qs.count) return;
+    const int keys = keys_held(p, s), past = keys - qs.count, first = i / p.block_rows * p.block_rows;
+    const Walk walk = walk_of<kStepKeys>(p, first, min(first + p.block_rows, qs.count) - 1, keys, past);
+    if (walk.count <= p.part_keys) return;
+    const int64_t at = partial_row(p, 0, head, s, i);
+    join_parts<T, E>(p.partial + at * E, partial_stats<E>(p) + at * 2, (int64_t)p.Hq * p.S * p.max_q, min((walk.count - 1) / p.part_keys + 1, p.parts), p.sl2,
+                     limit_of(p, i, keys, past) > 0, p.out + (int64_t)(qs.first + i) * p.out_token + head * p.out_head, lane);
+}
+
 // The numbered keys that a workgroup has at most: its rows' queries, at most max_q of them, see as many more than a window, in whole steps.
 static int most_numbered(int max_q, int max_k, int window, int sinks) {
     if (window == 0) return max_k;
-    const int64_t most = (int64_t)window + max_q + sinks + 2 * kStepKeys;
+    const int64_t most = (int64_t)window + max_q + sinks + 3 * kStepKeys;   // (the window, the first keys and the last in whole steps)
     return (int)std::min<int64_t>(most, max_k);
 }
 
@@ -673,16 +711,30 @@ constexpr PackedPrice kPagedPrices[2][2][kPagedForms] = {
     {{{16, 3.5f, 0.31f, 0.745f}, {32, 6.1f, 0.33f, 0.37f}, {64, 3.1f, 1.01f, 0.45f}, {128, 4.8f, 1.04f, 0.24f}},
      {{16, 2.7f, 0.36f, 1.78f}, {32, 6.9f, 0.39f, 0.72f}, {64, 5.9f, 0.84f, 0.61f}, {128, 5.85f, 1.18f, 0.38f}}}};
 constexpr float kPagedLast[2][2] = {{0.25f, 0.53f}, {0.235f, 0.56f}};
+// Rows of a head in parts: few of them over many keys leave CUs without work.  most_row_parts: by the room for their sums and by the keys, of any number of
+// queries within the limits.
+constexpr int64_t kMostRowPartBytes = 128 << 20;
+constexpr int kLeastRowPart = 1024;           // keys
+static int64_t row_part_bytes(int S, int Hq, int E, int max_q) { return (int64_t)S * Hq * max_q * (E + 2) * (int64_t)sizeof(float); }
+static int most_row_parts(int S, int Hq, int E, int max_q, int n) {
+    if ((int64_t)S * max_q > (1 << 20) || Hq > (1 << 12) || max_q < 32) return 1;
+    const int64_t workgroups = (int64_t)((max_q + 127) / 128) * Hq;   // of one sequence
+    const int64_t most = std::min<int64_t>({16, n / kLeastRowPart, 1024 / workgroups, kMostRowPartBytes / row_part_bytes(S, Hq, E, max_q)});
+    return (int)std::max<int64_t>(most, 1);
+}
 struct WholePlan {
     PackedForm form;
+    int parts;                // of the rows' forms
     double price;             // HUGE_VAL: no form's launch covers it
 };
-static WholePlan whole_plan(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int n, int causal, bool codes) {
-    WholePlan best{kKeys16, HUGE_VAL};
-    for (int f = 0; f < kPagedForms; f++) {
-        const double price = form_price((PackedForm)f, kPagedPrices[codes][E == 128][f], kPagedLast[codes][E == 128], S, Tq, Hq, Hk, max_q, n, causal);
-        if (price < best.price) best = WholePlan{(PackedForm)f, price};
-    }
+static WholePlan whole_plan(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int n, int causal, bool codes, int most_parts) {
+    WholePlan best{kKeys16, 1, HUGE_VAL};
+    for (int f = 0; f < kPagedForms; f++)
+        for (int parts = 1; parts <= (f >= kRows64 ? most_parts : 1); parts++) {
+            double price = form_price((PackedForm)f, kPagedPrices[codes][E == 128][f], kPagedLast[codes][E == 128], S, Tq, Hq, Hk, max_q, n, causal, parts);
+            if (parts > 1) price += 6.0 + (double)Tq * Hq * parts * E * 8 / 4e6;   // written and read again
+            if (price < best.price) best = WholePlan{(PackedForm)f, parts, price};
+        }
     return best;
 }
 static bool in_parts(const PartsPlan& parts, const WholePlan& whole) { return parts.few.rows > 0 && (parts.few.rows <= 32 || parts.price < whole.price); }
@@ -694,7 +746,9 @@ static int32_t launch_paged_rows(PagedParams p, hipStream_t stream) {
     if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return CHIPMUNK_ERR_LAUNCH;
     const PackedGrid grid = rows_grid(ROWS, p.S, p.Tq, p.Hq, p.Hk, p.max_q);
     p.tiles = (int)grid.tiles;
-    kernel<<<(uint32_t)grid.workgroups, 256, LDS, stream>>>(p);
+    p.block_rows = ROWS;
+    kernel<<<dim3((uint32_t)grid.workgroups, (uint32_t)p.parts), 256, LDS, stream>>>(p);
+    if (p.parts > 1) attn_paged_join_rows_kernel<T, E><<<dim3((uint32_t)(((int64_t)p.S * p.max_q + 3) / 4), (uint32_t)p.Hq), 256, 0, stream>>>(p);
     return launch_status();
 }
 
@@ -714,8 +768,8 @@ static int32_t launch_paged_few(PagedParams p, hipStream_t stream) {
 }
 
 template <class T, int E, bool CODES>
-static int32_t launch_paged(PagedParams p, const PartsPlan& parts, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
-    const WholePlan whole = whole_plan(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, n, p.causal, CODES);
+static int32_t launch_paged(PagedParams p, const PartsPlan& parts, int most_parts, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const WholePlan whole = whole_plan(p.S, p.Tq, p.Hq, p.Hk, E, p.max_q, n, p.causal, CODES, most_parts);
     if (in_parts(parts, whole)) {
         const FewPlan& few = parts.few;
         if (few_bytes(few, p.S, p.Hk, E) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
@@ -728,10 +782,13 @@ static int32_t launch_paged(PagedParams p, const PartsPlan& parts, int n, void* 
                                 : launch_paged_few<T, E, 4, CODES>(p, stream);
     }
     if (whole.price == HUGE_VAL) return CHIPMUNK_ERR_SHAPE;
-    if (whole.form <= kKeys32) {
-        p.few_rows = p.max_q * p.G;
-        p.part_keys = INT32_MAX;
-        p.parts = 1;
+    p.few_rows = p.max_q * p.G;
+    p.part_keys = INT32_MAX;
+    p.parts = whole.parts;
+    if (p.parts > 1) {
+        if ((size_t)(row_part_bytes(p.S, p.Hq, E, p.max_q) * p.parts) > (ws ? ws_bytes : 0)) return CHIPMUNK_ERR_WORKSPACE;
+        p.part_keys = (int)(((int64_t)n + (int64_t)p.parts * kStepKeys - 1) / ((int64_t)p.parts * kStepKeys) * kStepKeys);   // (whole steps)
+        p.partial = static_cast<float*>(ws);
     }
     switch (whole.form) {
         case kKeys16: return launch_paged_few<T, E, 1, CODES>(p, stream);
@@ -746,18 +803,20 @@ static int32_t launch_paged(PagedParams p, const PartsPlan& parts, int n, void* 
 using namespace chipmunk;
 
 
-// The form that a call takes and, for parts, their keys, for the tests.
+// The form that a call takes, with ten times its further parts, or the keys of a key head's parts, for the tests.
 extern "C" int chipmunk_internal_attn_paged_form(int S, int Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal, int window, int sinks, int codes) {
     const int n = most_numbered(max_q, max_k, window, sinks);
     const PartsPlan parts = parts_plan(S, Hq, Hk, E, max_q, n, codes != 0);
-    const WholePlan whole = whole_plan(S, Tq, Hq, Hk, E, std::min(max_q, Tq), n, causal, codes != 0);
-    return in_parts(parts, whole) ? parts.few.part_keys : whole.form;
+    const WholePlan whole = whole_plan(S, Tq, Hq, Hk, E, std::min(max_q, Tq), n, causal, codes != 0, most_row_parts(S, Hq, E, max_q, n));
+    return in_parts(parts, whole) ? parts.few.part_keys : whole.form + 10 * (whole.parts - 1);
 }
 
 extern "C" size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks) {
     if (S <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (E != 64 && E != 128) || max_q <= 0 || max_k <= 0 || window < 0 || sinks < 0) return 0;
     const int n = most_numbered(max_q, max_k, window, sinks);   // (of either format)
-    return std::max(few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, false).few, S, Hk, E), few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, true).few, S, Hk, E));
+    const int rows = most_row_parts(S, Hq, E, max_q, n);
+    return std::max({few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, false).few, S, Hk, E), few_bytes(parts_plan(S, Hq, Hk, E, max_q, n, true).few, S, Hk, E),
+                     rows > 1 ? (size_t)(row_part_bytes(S, Hq, E, max_q) * rows) : 0});
 }
 
 extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
@@ -791,11 +850,12 @@ extern "C" int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride
                   held, table, k_len, table_stride, most_keys, window, window ? sinks : 0, __builtin_ctz((uint32_t)held.page_size), 0};
     const int planned = most_numbered(max_q, most_keys, window, sinks);
     const PartsPlan parts = parts_plan_within(S, Hq, Hk, E, max_q, given, planned, held.format == CHIPMUNK_DTYPE_E4M3);
+    const int most_parts = std::min(most_row_parts(S, Hq, E, max_q, given), std::max(1, planned / kLeastRowPart));
     const auto st = static_cast<hipStream_t>(stream);
     auto go = [&](auto type, auto width) {
         typedef decltype(type) T;
         constexpr int W = decltype(width)::value;
-        return held.format == CHIPMUNK_DTYPE_E4M3 ? launch_paged<T, W, true>(p, parts, planned, ws, ws_bytes, st) : launch_paged<T, W, false>(p, parts, planned, ws, ws_bytes, st);
+        return held.format == CHIPMUNK_DTYPE_E4M3 ? launch_paged<T, W, true>(p, parts, most_parts, planned, ws, ws_bytes, st) : launch_paged<T, W, false>(p, parts, most_parts, planned, ws, ws_bytes, st);
     };
     typedef std::integral_constant<int, 64> Narrow;
     typedef std::integral_constant<int, 128> Wide;

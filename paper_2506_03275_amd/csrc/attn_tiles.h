@@ -349,16 +349,14 @@ __device__ __forceinline__ void store_joined(const AttnParams& p, int s, int hea
     }
 }
 
-// Joins the `parts` parts of a row of a key head, one wave's work.
+// Joins the `parts` parts of a row, one wave's work: sums, stats: those of the first part, `apart`: rows from one part's to the next's; to: its place.
 template <class T, int E>
-__device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head, int row, int first_query, int parts, bool sees, int lane) {
-    const float* sums = p.partial + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * E;
-    const float* stats = p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + (((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row) * 2;
+__device__ __forceinline__ void join_parts(const float* sums, const float* stats, int64_t apart, int parts, float sl2, bool sees, uint16_t* to, int lane) {
     constexpr int PER = E / 64;                           // columns of a lane
     constexpr int AHEAD = 8;
     float top = -INFINITY, total = 0.f, o[PER] = {};
     auto load = [&](int part, float (&v)[PER]) {
-        const float* from = sums + (int64_t)part * p.few_rows * E + lane * PER;
+        const float* from = sums + part * apart * E + lane * PER;
         if constexpr (PER == 2) {
             const f32x2 x = *reinterpret_cast<const f32x2*>(from);
             v[0] = x[0];
@@ -370,7 +368,7 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head,
     for (int part0 = 0; part0 < parts; part0 += 64) {     // 64 parts' references and sums at a time
         const int here = min(64, parts - part0);
         f32x2 mine = f32x2{-INFINITY, 0.f};
-        if (part0 + lane < parts) mine = *reinterpret_cast<const f32x2*>(stats + (int64_t)(part0 + lane) * p.few_rows * 2);
+        if (part0 + lane < parts) mine = *reinterpret_cast<const f32x2*>(stats + (part0 + lane) * apart * 2);
         float v[AHEAD][PER];                              // under way together with those
 #pragma unroll
         for (int n = 0; n < AHEAD; n++) load(part0 + min(n, here - 1), v[n]);
@@ -378,8 +376,8 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head,
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
         most = fmaxf(most, top);
-        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - most) * p.sl2);
-        const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[0] - most) * p.sl2);
+        const float before = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - most) * sl2);
+        const float weight = mine[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine[0] - most) * sl2);
         float add = mine[1] * weight;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) add += __shfl_xor(add, d);
@@ -405,12 +403,20 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head,
     }
     // a row that sees no key has no weight anywhere
     const float f = sees ? 1.f / total : 0.f;
-    uint16_t* to = p.out + (int64_t)(first_query + row / p.G) * p.out_token + (head * p.G + row % p.G) * p.out_head + lane * PER;
+    to += lane * PER;
     if constexpr (PER == 2) {
         *reinterpret_cast<uint32_t*>(to) = T::pack(o[0] * f, o[PER - 1] * f);
     } else {
         *to = (uint16_t)T::pack(o[0] * f, 0.f);
     }
+}
+
+// The same of a row of a key head, where store_joined left its parts.
+template <class T, int E>
+__device__ __forceinline__ void join_parts(const AttnParams& p, int s, int head, int row, int first_query, int parts, bool sees, int lane) {
+    const int64_t first = ((int64_t)s * p.Hk + head) * p.parts * p.few_rows + row;
+    join_parts<T, E>(p.partial + first * E, p.partial + (int64_t)p.S * p.Hk * p.parts * p.few_rows * E + first * 2, p.few_rows, parts, p.sl2, sees,
+                     p.out + (int64_t)(first_query + row / p.G) * p.out_token + (head * p.G + row % p.G) * p.out_head, lane);
 }
 
 // Tiles (of a head, or of a sequence and key head) and workgroups of a launch: in double precision, for sizes that no launch covers.
@@ -497,11 +503,11 @@ constexpr PackedPrice kPackedPrices[2][kPackedForms] = {{{16, 3.8f, 0.17f, 0.81f
                                                            {{16, 5.5f, 0.165f, 1.78f}, {32, 8.3f, 0.43f, 0.70f}, {64, 5.1f, 0.94f, 0.64f}, {128, 5.1f, 1.49f, 0.50f}, {192, 13.8f, 2.34f, 0.41f}}};
 constexpr float kPackedLast[2][2] = {{0.35f, 0.25f}, {0.49f, 0.53f}};   // of E = 64, 128; all keys, causal
 constexpr double kPackedEmpty = 0.0008;               // us
-// last_share: of the last workgroup
-inline double form_price(PackedForm form, const PackedPrice& f, double last_share, int S, int64_t Tq, int Hq, int Hk, int max_q, int max_k, int causal) {
+// last_share: of the last workgroup; parts: in which every workgroup's keys are divided
+inline double form_price(PackedForm form, const PackedPrice& f, double last_share, int S, int64_t Tq, int Hq, int Hk, int max_q, int max_k, int causal, int parts = 1) {
     const bool grouped = form <= kKeys32;                 // rows of a key head, of all its queries' heads
     const double launched = (grouped ? few_grid(f.rows, S, Hk, (int64_t)max_q * (Hq / Hk), 1) : rows_grid(f.rows, S, Tq, Hq, Hk, max_q)).workgroups;
-    if (launched >= kMostWorkgroups) return HUGE_VAL;
+    if (launched * parts >= kMostWorkgroups) return HUGE_VAL;
     const double per_query = grouped ? (double)Hq / Hk : 1.0, heads = grouped ? Hk : Hq;
     double workgroups = 0, units = 0;
     const double rest = S > 1 ? std::max(0.0, (double)(Tq - max_q) / (S - 1)) : 0.0;
@@ -513,8 +519,9 @@ inline double form_price(PackedForm form, const PackedPrice& f, double last_shar
     };
     add(1, max_q, max_k);
     if (S > 1) add(S - 1, rest, rest * max_k / max_q);
-    const double longest = max_k / 64.0, last = last_share * longest * (f.rows / 64.0) * f.full;
-    return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last) + kPackedEmpty * std::max(0.0, launched - workgroups);
+    const double longest = max_k / 64.0 / parts, last = last_share * longest * (f.rows / 64.0) * f.full;
+    workgroups *= parts;
+    return f.start * std::max(1.0, workgroups / 512) + std::max(longest * f.alone, units / 256 * f.full + last) + kPackedEmpty * std::max(0.0, launched * parts - workgroups);
 }
 inline double packed_price(PackedForm form, int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int max_k, int causal) {
     return form_price(form, kPackedPrices[E == 128][form], kPackedLast[E == 128][causal != 0], S, Tq, Hq, Hk, max_q, max_k, causal);

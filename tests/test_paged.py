@@ -273,6 +273,11 @@ DIVIDED = [(128, 0, 512, 1, 1, [33], [6276]), (128, 0, 1024, 8, 8, [33, 1, 0, 20
            (64, 0, 768, 4, 4, [65, 2, 3, 65], [7586, 7000, 1, 300]), (64, 1, 1024, 4, 4, [130, 9, 1, 2], [8589, 1024, 1025, 3000]), (64, 1, 512, 1, 1, [33], [2378])]
 
 
+# and rows of a head over keys in parts: E, codes, parts, Hq, Hk, nq, nk
+ROWS_DIVIDED = [(128, 0, 4, 8, 1, [300, 7], [6000, 4097]), (128, 1, 4, 8, 1, [300, 1, 0, 299], [6100, 1024, 70, 1025]), (64, 0, 5, 16, 2, [200], [9001]), (64, 1, 5, 16, 2, [200, 150], [9000, 5000]),
+                (128, 1, 16, 8, 1, [130], [40000]), (64, 0, 16, 9, 1, [129], [20011])]
+
+
 def _form(cm, E, Hq, Hk, nq, nk, codes, window=0, sinks=0, causal=1):
     Tq = len(nq) * max(nq) if nk is not nq else sum(nq)
     return cm.load().chipmunk_internal_attn_paged_form(len(nq), Tq, Hq, Hk, E, max(nq), max(nk), causal, window, sinks, codes)
@@ -302,6 +307,19 @@ def test_many_rows_over_divided_keys(cm, E, codes, keys, Hq, Hk, nq, nk):
         q[:b.q.shape[0]] = b.q
         b.q = q
         for window, sinks in ((0, 0), (2000, 40)):
+            b.check(True, None, window, sinks)
+        b.check(False)
+
+
+@gpu
+@pytest.mark.parametrize("E,codes,parts,Hq,Hk,nq,nk", ROWS_DIVIDED)
+def test_rows_over_divided_keys(cm, E, codes, parts, Hq, Hk, nq, nk):
+    for dtype in TYPES:
+        b = Batch(cm, nq, nk, Hq, Hk, E, dtype, E4M3 if codes else dtype, 64, seed=parts)
+        q = torch.zeros((len(nq) * max(nq), Hq, E), dtype=dtype, device=DEV)
+        q[:b.q.shape[0]] = b.q
+        b.q = q
+        for window, sinks in ((0, 0), (max(nk) - 1500, 100), (3000, 0)):
             b.check(True, None, window, sinks)
         b.check(False)
 
