@@ -651,9 +651,9 @@ static int most_numbered(int max_q, int max_k, int window, int sinks) {
 }
 
 // Up to 1024 rows of a key head may walk their n numbered keys in parts, whose length goes by its price.  A part of codes takes half the time to begin and end
-// that one of elements does.  Measured on 4009 batches of up to 32 rows (1 to 128 sequences of 300 to 40 000 keys, ragged and not) and 5294 of more (1 to 8
-// sequences, with windows and without): parts or whole, and their length, take 1.03 times the quickest's time in the mean in either, of
-// codes and of elements (by the rules of packed attention 1.06 and 1.04; 1.07 and 1.05; 6.5 at most).
+// that one of elements does.  Measured on 4009 batches of up to 32 rows (1 to 128 sequences of 300 to 40 000 keys, ragged and not): parts or whole, and
+// their length, take 1.03 times the quickest's time in the mean, of codes and of elements (by the rules of packed attention 1.06 and 1.04).  More rows
+// have their price beside whole_plan's.
 struct PartsPlan {
     FewPlan few;              // rows 0: none
     double price;             // us; of more than 32 rows
@@ -661,8 +661,8 @@ struct PartsPlan {
 struct PartsPrice {
     float start, keys, join, join_block, share;   // of a launch; 64 keys of 64 rows; a part's joining, for each block of 64 rows; workgroups that have work
 };
-constexpr PartsPrice kPartsPrices[2][2] = {{{6.f, 0.5f, 0.073f, 0.002f, 0.71f}, {14.f, 0.66f, 0.38f, 0.0015f, 0.89f}},   // elements: E = 64, 128
-                                           {{6.5f, 0.62f, 0.17f, 0.0008f, 0.56f}, {6.8f, 0.9f, 0.17f, 0.002f, 1.1f}}};   // codes
+constexpr PartsPrice kPartsPrices[2][2] = {{{6.5f, 0.615f, 0.074f, 0.0074f, 1.47f}, {16.3f, 0.567f, 0.167f, 0.0035f, 1.65f}},   // elements: E = 64, 128
+                                           {{8.8f, 0.423f, 0.092f, 0.006f, 1.4f}, {8.1f, 0.8f, 0.17f, 0.004f, 1.59f}}};         // codes
 constexpr int64_t kMostPartRows = 1 << 19;    // rows of all parts in the workspace, of more than 32 rows (272 MB at E = 128)
 static PartsPlan parts_plan(int S, int Hq, int Hk, int E, int max_q, int n, bool codes) {
     const PartsPlan none{FewPlan{0, 0, 0}, HUGE_VAL};
@@ -711,16 +711,25 @@ constexpr PackedPrice kPagedPrices[2][2][kPagedForms] = {
     {{{16, 3.5f, 0.31f, 0.745f}, {32, 6.1f, 0.33f, 0.37f}, {64, 3.1f, 1.01f, 0.45f}, {128, 4.8f, 1.04f, 0.24f}},
      {{16, 2.7f, 0.36f, 1.78f}, {32, 6.9f, 0.39f, 0.72f}, {64, 5.9f, 0.84f, 0.61f}, {128, 5.85f, 1.18f, 0.38f}}}};
 constexpr float kPagedLast[2][2] = {{0.25f, 0.53f}, {0.235f, 0.56f}};
-// Rows of a head in parts: few of them over many keys leave CUs without work.  most_row_parts: by the room for their sums and by the keys, of any number of
-// queries within the limits.
-constexpr int64_t kMostRowPartBytes = 128 << 20;
-constexpr int kLeastRowPart = 1024;           // keys
+// Rows of a head in parts of their keys: few of them over many keys leave CUs without work (one chunk of 512 tokens, 32 heads, over 32 768 keys: 430 us whole).
+// Joined are Tq Hq rows, from 1 MB of sums on by their size.  Over 1581 batches of 40 to 2048 queries of 1 to 4 sequences over 1500 to 60 000 keys what
+// is taken, whole, rows or a key head's rows in parts, takes 1.05 (E = 64) and 1.07 times the quickest's time in the mean; without rows in parts 1.17 to 1.22.
+struct RowPartsPrice {
+    PackedPrice forms[2];     // 64 and 128 rows
+    float last, join, join_mb;
+};
+constexpr RowPartsPrice kRowPartsPrices[2][2] = {{{{{64, 1.96f, 0.9f, 0.295f}, {128, 3.63f, 2.08f, 0.141f}}, 0.124f, 4.2f, 0.116f},     // elements: E = 64, 128
+                                                  {{{64, 8.4f, 0.86f, 0.61f}, {128, 7.8f, 1.97f, 0.242f}}, 0.66f, 6.f, 0.25f}},
+                                                 {{{{64, 2.4f, 0.84f, 0.33f}, {128, 2.f, 1.3f, 0.242f}}, 0.089f, 2.8f, 0.26f},          // codes
+                                                  {{{64, 5.9f, 0.84f, 0.61f}, {128, 3.9f, 1.49f, 0.387f}}, 0.63f, 4.8f, 0.165f}}};
+constexpr int64_t kMostRowPartBytes = 64 << 20;
+constexpr int kLeastRowPart = 512, kMostRowParts = 16;   // keys; parts
 static int64_t row_part_bytes(int S, int Hq, int E, int max_q) { return (int64_t)S * Hq * max_q * (E + 2) * (int64_t)sizeof(float); }
+// The parts that there may be, by the room for their sums, by the keys and by the CUs, of any number of queries within the limits.
 static int most_row_parts(int S, int Hq, int E, int max_q, int n) {
     if ((int64_t)S * max_q > (1 << 20) || Hq > (1 << 12) || max_q < 32) return 1;
     const int64_t workgroups = (int64_t)((max_q + 127) / 128) * Hq;   // of one sequence
-    const int64_t most = std::min<int64_t>({16, n / kLeastRowPart, 1024 / workgroups, kMostRowPartBytes / row_part_bytes(S, Hq, E, max_q)});
-    return (int)std::max<int64_t>(most, 1);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kMostRowParts, n / kLeastRowPart, 1024 / workgroups, kMostRowPartBytes / row_part_bytes(S, Hq, E, max_q)}));
 }
 struct WholePlan {
     PackedForm form;
@@ -729,10 +738,16 @@ struct WholePlan {
 };
 static WholePlan whole_plan(int S, int64_t Tq, int Hq, int Hk, int E, int max_q, int n, int causal, bool codes, int most_parts) {
     WholePlan best{kKeys16, 1, HUGE_VAL};
-    for (int f = 0; f < kPagedForms; f++)
-        for (int parts = 1; parts <= (f >= kRows64 ? most_parts : 1); parts++) {
-            double price = form_price((PackedForm)f, kPagedPrices[codes][E == 128][f], kPagedLast[codes][E == 128], S, Tq, Hq, Hk, max_q, n, causal, parts);
-            if (parts > 1) price += 6.0 + (double)Tq * Hq * parts * E * 8 / 4e6;   // written and read again
+    for (int f = 0; f < kPagedForms; f++) {
+        const double price = form_price((PackedForm)f, kPagedPrices[codes][E == 128][f], kPagedLast[codes][E == 128], S, Tq, Hq, Hk, max_q, n, causal);
+        if (price < best.price) best = WholePlan{(PackedForm)f, 1, price};
+    }
+    const RowPartsPrice& r = kRowPartsPrices[codes][E == 128];
+    for (int f = kRows64; f < kPagedForms; f++)
+        for (int parts : {2, 3, 4, 6, 8, 12, 16}) {
+            if (parts > most_parts) break;
+            const double price = form_price((PackedForm)f, r.forms[f - kRows64], r.last, S, Tq, Hq, Hk, max_q, n, causal, parts) + r.join +
+                                 (double)Tq * Hq * parts * E * 8 / 1e6 * r.join_mb;
             if (price < best.price) best = WholePlan{(PackedForm)f, parts, price};
         }
     return best;

@@ -269,13 +269,12 @@ FORMS = [(128, 0, 0, 1, 1, [43, 6, 20, 32]), (128, 0, 1, 2, 2, [2761]), (128, 0,
          (64, 0, 0, 1, 1, [101]), (64, 0, 1, 8, 8, [1572, 6]), (64, 0, 2, 1, 1, [38, 20, 35, 8]), (64, 0, 3, 32, 8, [1937, 1884]),
          (64, 1, 0, 1, 1, [101]), (64, 1, 1, 8, 8, [1482, 105, 5, 25]), (64, 1, 2, 1, 1, [30, 7, 6, 14, 29, 15]), (64, 1, 3, 40, 8, [360, 138, 194, 64, 228, 37])]
 # and of more than 32 rows of a key head over keys in parts: E, codes, keys of a part, Hq, Hk, nq, nk
-DIVIDED = [(128, 0, 512, 1, 1, [33], [6276]), (128, 0, 1024, 8, 8, [33, 1, 0, 20, 33, 7], [5404, 5000, 3, 1025, 40, 7]), (128, 1, 512, 1, 1, [35], [2775]), (128, 1, 768, 4, 4, [71, 70, 1, 60], [5156, 4000, 769, 768]),
-           (64, 0, 768, 4, 4, [65, 2, 3, 65], [7586, 7000, 1, 300]), (64, 1, 1024, 4, 4, [130, 9, 1, 2], [8589, 1024, 1025, 3000]), (64, 1, 512, 1, 1, [33], [2378])]
-
-
-# and rows of a head over keys in parts: E, codes, parts, Hq, Hk, nq, nk
-ROWS_DIVIDED = [(128, 0, 4, 8, 1, [300, 7], [6000, 4097]), (128, 1, 4, 8, 1, [300, 1, 0, 299], [6100, 1024, 70, 1025]), (64, 0, 5, 16, 2, [200], [9001]), (64, 1, 5, 16, 2, [200, 150], [9000, 5000]),
-                (128, 1, 16, 8, 1, [130], [40000]), (64, 0, 16, 9, 1, [129], [20011])]
+DIVIDED = [(128, 0, 512, 1, 1, [37], [5314]), (128, 0, 1536, 4, 4, [88, 1, 0, 80], [7550, 1537, 3, 7000]), (128, 1, 512, 1, 1, [33], [2251]), (128, 1, 768, 4, 4, [65, 64, 1, 60], [3689, 3600, 769, 768]),
+           (64, 0, 768, 2, 2, [65, 2, 3, 65, 0, 9], [5758, 5000, 1, 300, 70, 769]), (64, 1, 1024, 20, 4, [181], [3011]), (64, 1, 512, 1, 1, [35], [2251])]
+# and 64 or 128 rows of a head over keys in parts: E, codes, ten times the further parts and the form, Hq, Hk, nq, nk
+ROWS_DIVIDED = [(128, 0, 52, 8, 1, [300, 7], [6000, 4097]), (128, 1, 53, 8, 1, [300, 1, 0, 299], [6100, 1024, 70, 1025]), (64, 0, 112, 16, 2, [200], [9001]), (64, 1, 113, 16, 2, [200, 150], [9000, 5000]),
+                (128, 1, 152, 8, 1, [130], [40000]), (64, 0, 152, 9, 1, [129], [20011]), (128, 0, 72, 8, 8, [33, 1, 0, 20, 33, 7], [5404, 5000, 3, 1025, 40, 7]),
+                (64, 1, 112, 4, 4, [130, 9, 1, 2], [8589, 1024, 1025, 3000])]
 
 
 def _form(cm, E, Hq, Hk, nq, nk, codes, window=0, sinks=0, causal=1):
@@ -288,6 +287,8 @@ def test_the_forms_are_what_the_batches_take(cm):
         assert _form(cm, E, Hq, Hk, lengths, lengths, codes) == form == _form(cm, E, Hq, Hk, lengths, lengths, codes, 150, 70)
     for E, codes, keys, Hq, Hk, nq, nk in DIVIDED:
         assert _form(cm, E, Hq, Hk, nq, nk, codes) == keys and max(nq) * Hq // Hk > 32
+    for E, codes, form, Hq, Hk, nq, nk in ROWS_DIVIDED:
+        assert _form(cm, E, Hq, Hk, nq, nk, codes) == form
 
 
 @gpu
@@ -312,10 +313,10 @@ def test_many_rows_over_divided_keys(cm, E, codes, keys, Hq, Hk, nq, nk):
 
 
 @gpu
-@pytest.mark.parametrize("E,codes,parts,Hq,Hk,nq,nk", ROWS_DIVIDED)
-def test_rows_over_divided_keys(cm, E, codes, parts, Hq, Hk, nq, nk):
+@pytest.mark.parametrize("E,codes,form,Hq,Hk,nq,nk", ROWS_DIVIDED)
+def test_rows_over_divided_keys(cm, E, codes, form, Hq, Hk, nq, nk):
     for dtype in TYPES:
-        b = Batch(cm, nq, nk, Hq, Hk, E, dtype, E4M3 if codes else dtype, 64, seed=parts)
+        b = Batch(cm, nq, nk, Hq, Hk, E, dtype, E4M3 if codes else dtype, 64, seed=form)
         q = torch.zeros((len(nq) * max(nq), Hq, E), dtype=dtype, device=DEV)
         q[:b.q.shape[0]] = b.q
         b.q = q
