@@ -356,7 +356,7 @@ int32_t chipmunk_norm_rope_grad(const uint16_t* grad, int64_t grad_token_stride,
 /* ---- Keys and values of many sequences in pages of page_size tokens each.  Row r of the pages is token r % page_size of page
  * r / page_size.  The elements are of the calls' type, or e4m3 (OCP: 4 exponent bits, 3 of the fraction) under a power of two for
  * each row of a head: the row stands for code * 2^(scale - 127), rounded to the calls' type.  A power of two costs e4m3 nothing
- * but range and makes the way back exact. ---- */
+ * but range and makes the way back exact.  A scale of 255, which no write gives, is a NaN. ---- */
 
 #define CHIPMUNK_DTYPE_E4M3  2   /* of pages only */
 
@@ -371,7 +371,7 @@ typedef struct {
     int32_t format;                       /* CHIPMUNK_DTYPE_*: that of the calls, or E4M3 */
 } chipmunk_pages;
 
-/* Writes keys and values of new tokens to their rows of the pages.  k, v: [tokens, heads, E], any strides of rows that do not overlap;
+/* Writes keys and values of new tokens to their rows of the pages.  k, v: [tokens, heads, E], any strides of rows that do not overlap, not in the pages;
  * rows: int64 [tokens]; a token whose row is negative, or behind the last page, is not written.  No row may be named twice: what it then
  * holds is undefined (of that row alone).
  * e4m3: 2^k, k = scale - 127, is the least power at which the row's largest magnitude is 448 at most (k >= -126; a row of zeros: 0);
@@ -380,7 +380,7 @@ typedef struct {
 int32_t chipmunk_cache_write(const uint16_t* k, int64_t k_token_stride, int64_t k_head_stride, const uint16_t* v, int64_t v_token_stride,
                              int64_t v_head_stride, const int64_t* rows, const chipmunk_pages* pages, int tokens, int dtype, void* stream);
 
-/* Rows of the pages back as elements: k, v: [tokens, heads, E], any strides of rows that do not overlap.  Rows may be named more than once;
+/* Rows of the pages back as elements: k, v: [tokens, heads, E], any strides of rows that do not overlap, not in the pages.  Rows may be named more than once;
  * where one is negative, or behind the last page, k and v are left as they are. */
 int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_t* rows, uint16_t* k, int64_t k_token_stride, int64_t k_head_stride, uint16_t* v,
                             int64_t v_token_stride, int64_t v_head_stride, int tokens, int dtype, void* stream);

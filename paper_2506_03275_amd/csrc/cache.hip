@@ -1,7 +1,8 @@
 // Keys and values of new tokens into pages, and rows of pages back: in the element type, copied, or in e4m3 with a power of two for each row of a
 // head (pages.h has the numbers).
 //
-// Bound: memory; a row of a head in e4m3 is 2 E bytes on one side and E + 1 on the other.
+// Bound: memory; a row of a head in e4m3 is 2 E bytes on one side and E + 1 on the other.  16 383 tokens of 8 heads x 128 written in 21 us and read in 17 (4.8
+// and 6.1 TB/s), 75 600 of 24 heads read in 257 (5.4 TB/s); 16 tokens 3.0 and 2.8 us.
 #include "pages.h"
 #include "rope.h"
 
