@@ -373,7 +373,7 @@ typedef struct {
 
 /* Writes keys and values of new tokens to their rows of the pages.  k, v: [tokens, heads, E], any strides of rows that do not overlap, not in the pages;
  * rows: int64 [tokens]; a token whose row is negative, or behind the last page, is not written.  No row may be named twice: what it then
- * holds is undefined (of that row alone).
+ * holds is undefined (of that row alone).  Here and in reading tokens * heads * E < 2^35 - 2048.
  * e4m3: 2^k, k = scale - 127, is the least power at which the row's largest magnitude is 448 at most (k >= -126; a row of zeros: 0);
  * code = x 2^-k rounded to nearest even.  Infinities and NaN become NaN and do not count for the power; magnitudes above 1.875 * 2^127 (fp16:
  * 1.875 * 2^15) are taken as that, so that no value comes back infinite. */
@@ -396,7 +396,7 @@ int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_t* rows, ui
  * else; its rows that belong to no sequence are left as they were.  table: int32 [S][table_pages], row stride table_stride; entries behind a
  * sequence's last page are not read; a page that the pages do not have reads as zeros.  max_q, max_k: no sequence has more queries, keys;
  * sequences that do are cut there, which gives wrong results, as do bad entries of cu_q and k_len, without accesses outside the tensors.
- * They may be far too large.  table_pages * page_size <= 2^30; softmax_scale in (0, 2^127]; token strides < 2^24.
+ * They may be far too large.  table_pages * page_size <= 2^30; softmax_scale in (0, 2^127]; token strides < 2^24; (Tq / 128 + S + 8) * Hq < 2^24.
  * ws: chipmunk_attn_paged_workspace_bytes() (0: ws may be NULL; also 0 on bad arguments) of the same sizes, contents undefined afterwards,
  * not to be shared by calls that may overlap. */
 size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks);
