@@ -106,15 +106,14 @@ struct NormItem {
             f[b] = u * sn + v * c[i];
         }
     }
-    // A row's x becomes n = x r; r.  Squares of bf16 may pass 32 bits' range: then they are taken of values 2^-72 times as large, whose eps is lost
-    // beside them.
+    // A row's x becomes n = x r; r.  Squares of bf16, and their mean with eps, may pass 32 bits' range: then n is formed of values 2^-72 times as large,
+    // and so is the root (eps counts there too: beside a mean of 2^119 or more, which a sum of 2^128 leaves, any up to 2^128 may stand).
     __device__ __forceinline__ static float normalize(const NormParams& p, float (&f)[NE]) {
         float sum = 0.f, down = 1.f;
 #pragma unroll
         for (int i = 0; i < NE; i++) sum += f[i] * f[i];
-        sum = row_sum(sum, p.lanes);
-        float r = __builtin_amdgcn_rsqf(sum * p.inv_E + p.eps);
-        if ((__float_as_uint(sum) & 0x7f800000u) == 0x7f800000u) {
+        float mean = row_sum(sum, p.lanes) * p.inv_E + p.eps;
+        if ((__float_as_uint(mean) & 0x7f800000u) == 0x7f800000u) {
             down = 0x1p-72f;
             sum = 0.f;
 #pragma unroll
@@ -122,8 +121,9 @@ struct NormItem {
                 f[i] *= down;
                 sum += f[i] * f[i];
             }
-            r = __builtin_amdgcn_rsqf(row_sum(sum, p.lanes) * p.inv_E);
+            mean = row_sum(sum, p.lanes) * p.inv_E + p.eps * down * down;
         }
+        const float r = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
         for (int i = 0; i < NE; i++) f[i] *= r;
         return r * down;

@@ -205,6 +205,27 @@ def test_rows_of_zeros_and_of_extremes(cm, halves):
 
 
 @gpu
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("size,eps", [(2.0 ** 61, 1e37), (1.2e18, 3.4e38), (3e19, 3e38), (1.0, 3.4e38), (2.0 ** 61, 1e-6)])
+def test_squares_beyond_32_bits_beside_an_eps_of_their_size(cm, size, eps, halves):
+    """The sum of a row's squares, or their mean and eps together, pass 32 bits' range (1.2e18: the latter alone): eps counts all the same."""
+    axes = (16, 8, 8)
+    x, wq, wk, pos, freqs, rows, r = _inputs(cm, 6, 3, 64, axes, torch.bfloat16, 7)
+    x.copy_(torch.where(x < 0, -size, size) * (1 + 0.1 * torch.rand(x.shape, device=DEV)))
+    x[4] = r(3, 64)                                             # (a row as any)
+    out = rows()
+    cm.norm_rope(x, wq, wk, 2, pos, freqs, out, axes, eps, halves)
+    want, off = norm_rope_reference(x, wq, wk, 2, pos, freqs, axes, eps, halves)
+    assert bool(((out.double() - want).abs() <= off).all())
+    grad, dx, dw = r(6, 3, 64).to(torch.bfloat16), rows(), torch.empty((2, 64), device=DEV)
+    ws = torch.empty(cm.norm_rope_grad_workspace_bytes(6, 3, 64), dtype=torch.uint8, device=DEV)
+    cm.norm_rope_grad(grad, x, wq, wk, 2, pos, freqs, dx, dw[0], dw[1], axes, eps, halves, ws)
+    want, weights, off, slack = norm_rope_grad_reference(grad, x, wq, wk, 2, pos, freqs, axes, eps, halves)
+    assert bool(((dx.double() - want).abs() <= off).all())
+    assert all(bool(((got.double() - exact).abs() <= most).all()) for got, exact, most in zip(dw, weights, slack))
+
+
+@gpu
 def test_one_weight_alone(cm):
     """Where no head has a weight there need not be one."""
     x, w, other, pos, freqs, rows, r = _inputs(cm, 20, 3, 64, (32, 0, 0), torch.bfloat16, 2)
