@@ -368,7 +368,7 @@ static int32_t norm_call(NormParams& p, bool grad, int64_t pairs_t, int64_t pair
     p.end1 = (int)(pairs_t + pairs_h);
     p.pairs = (int)pairs;
     p.inv_E = 1.f / (float)p.E;
-    const NormGrid g = norm_grid(p.tokens, p.heads, p.E, pairs, halves != 0, p.out_head > p.out_token, grad);
+    const NormGrid g = norm_grid(p.tokens, p.heads, p.E, pairs, halves != 0, p.tokens > 1 && p.out_head > p.out_token, grad);
     p.items = g.items;
     p.lanes = g.lanes;
     p.side = g.side;

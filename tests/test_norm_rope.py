@@ -156,6 +156,23 @@ def test_gradient(cm, tokens, heads, q_heads, E, axes, halves):
 
 @gpu
 @pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("heads,E", [(40, 128), (100, 64), (5, 128)])
+def test_one_token_is_summed_as_the_first_of_two(cm, heads, E, halves):
+    """A token alone has no stride that could tell rows from heads of rows: its rows' sums are those of a second one behind it whose gradient is zero."""
+    axes, dw = (E // 2, 0, 0), []
+    x, wq, wk, pos, freqs, rows, r = _inputs(cm, 2, heads, E, axes, torch.bfloat16, 4)
+    grad = rows(r(2, heads, E).to(torch.bfloat16))
+    grad[1] = 0
+    ws = torch.empty(cm.norm_rope_grad_workspace_bytes(2, heads, E), dtype=torch.uint8, device=DEV)
+    for n in (2, 1):
+        dx = torch.empty((n, heads, E), dtype=torch.bfloat16, device=DEV)
+        dw.append((dx[0], torch.empty((2, E), device=DEV)))
+        cm.norm_rope_grad(grad[:n], x[:n], wq, wk, heads // 2, pos[:n], freqs, dx, dw[-1][1][0], dw[-1][1][1], axes, 1e-6, halves, ws)
+    assert torch.equal(dw[0][0], dw[1][0]) and torch.equal(dw[0][1], dw[1][1])
+
+
+@gpu
+@pytest.mark.parametrize("halves", [False, True])
 def test_gradient_against_differences(cm, halves):
     """The loss sum(c out) over single steps of x and of a weight: differences of the definition in 64 bits against the kernel's gradients."""
     axes, dtype, eps = (8, 16, 8), torch.float16, 1e-3
