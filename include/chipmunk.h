@@ -343,9 +343,9 @@ int32_t chipmunk_norm_rope(const uint16_t* x, int64_t x_token_stride, int64_t x_
 
 /* Its gradient.  grad: of out; x: as chipmunk_norm_rope had it.  With g = turn^-1(grad), n = x r, c = mean_e(g_e w_e n_e):
  *   dx[t,h] = r (g w - n c);   dq_weight[e], dk_weight[e] = sum of g_e n_e over the tokens and the heads that have the weight
- * (fp32 [E], written; NULL where no head has it; a sum's order depends on the sizes alone).  dx may be grad or x (same pointer and
- * strides) and overlaps nothing else.  ws: chipmunk_norm_rope_grad_workspace_bytes() (0 on bad arguments), contents undefined
- * afterwards, not to be shared by calls that may overlap. */
+ * (fp32 [E], written; NULL where no head has it).  A sum's order depends on the sizes, on halves and on which of dx's two strides is the
+ * larger, and on nothing else: a call repeated gives the same bits.  dx may be grad or x (same pointer and strides) and overlaps nothing else.
+ * ws: chipmunk_norm_rope_grad_workspace_bytes() (0 on bad arguments), contents undefined afterwards, not to be shared by calls that may overlap. */
 size_t chipmunk_norm_rope_grad_workspace_bytes(int tokens, int heads, int E);
 int32_t chipmunk_norm_rope_grad(const uint16_t* grad, int64_t grad_token_stride, int64_t grad_head_stride, const uint16_t* x, int64_t x_token_stride,
                                 int64_t x_head_stride, const uint16_t* q_weight, const uint16_t* k_weight, int q_heads, const int32_t* pos,

@@ -180,8 +180,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p) {
     }
 }
 
-// The weights' gradients are summed in 32 bits in an order that the sizes alone decide: a thread's rows, the rows that a workgroup's threads
-// have side by side, then the workgroups (norm_weights_kernel).
+// The weights' gradients are summed in 32 bits in an order that the launch's layout decides, and that goes by the sizes, HALVES and whether dx is heads of
+// rows alone: a thread's rows, the rows that a workgroup's threads have side by side, then the workgroups (norm_weights_kernel).  (One layout for
+// either dx would make it one order: 18 000 x 80 heads x 128 as rows 200 -> 227 us, or as heads of rows 218 -> 232, of 64 126 -> 159.)
 template <class T, bool HALVES, int SOURCE, int RESULT>
 __global__ __launch_bounds__(kNormThreads) void norm_rope_grad_kernel(NormParams p) {
     typedef NormItem<T, HALVES> Item;

@@ -156,6 +156,31 @@ def test_gradient(cm, tokens, heads, q_heads, E, axes, halves):
 
 @gpu
 @pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("tokens,heads", [(1, 40), (8, 40), (333, 48), (4608, 48), (12011, 90)])
+def test_what_the_order_of_the_weights_sums_goes_by(cm, tokens, heads, halves):
+    """Sizes, halves and which of dx's strides is the larger: where x and grad lie, what is between dx's rows and the alignment of a row change no bit of
+    the weights' gradients, and nothing changes dx.  Each of dx's two orders is compared with 64 bits (test_gradient has one for the largest size)."""
+    axes, E, got = (16, 24, 24), 128, {}
+    for order, layouts in (("rows", ("rows", "projection", "rows of 136")), ("heads", ("heads", "heads of 136"))):
+        for to, source in zip(layouts, ("rows", "heads", "projection")):
+            x, wq, wk, pos, freqs, rows, r = _inputs(cm, tokens, heads, E, axes, torch.bfloat16, 11, source)
+            grad, dw = rows(r(tokens, heads, E).to(torch.bfloat16)), torch.full((2, E), math.nan, device=DEV)
+            wide = to.endswith("136")
+            dx = torch.empty((heads, tokens, 136), dtype=x.dtype, device=DEV).transpose(0, 1)[..., 8:] if wide and order == "heads" else (
+                torch.empty((tokens, heads, 136), dtype=x.dtype, device=DEV)[..., 8:] if wide else _inputs(cm, tokens, heads, E, axes, x.dtype, 0, to)[5]())
+            ws = torch.full((cm.norm_rope_grad_workspace_bytes(tokens, heads, E),), 255, dtype=torch.uint8, device=DEV)
+            cm.norm_rope_grad(grad, x, wq, wk, heads // 2, pos, freqs, dx, dw[0], dw[1], axes, 1e-6, halves, ws)
+            if order not in got:
+                want, weights, off, slack = norm_rope_grad_reference(grad, x, wq, wk, heads // 2, pos, freqs, axes, 1e-6, halves)
+                assert bool(((dx.double() - want).abs() <= off).all()), order
+                assert all(bool(((d.double() - exact).abs() <= most).all()) for d, exact, most in zip(dw, weights, slack)), order
+                got[order] = dw
+            got["dx"] = got.get("dx", dx)
+            assert torch.equal(dx, got["dx"]) and torch.equal(dw, got[order]), to
+
+
+@gpu
+@pytest.mark.parametrize("halves", [False, True])
 @pytest.mark.parametrize("heads,E", [(40, 128), (100, 64), (5, 128)])
 def test_one_token_is_summed_as_the_first_of_two(cm, heads, E, halves):
     """A token alone has no stride that could tell rows from heads of rows: its rows' sums are those of a second one behind it whose gradient is zero."""
