@@ -398,7 +398,8 @@ int32_t chipmunk_cache_read(const chipmunk_pages* pages, const int64_t* rows, ui
  * sequences that do are cut there, which gives wrong results, as do bad entries of cu_q and k_len, without accesses outside the tensors.
  * They may be far too large.  table_pages * page_size <= 2^30; softmax_scale in (0, 2^127]; token strides < 2^24; (Tq / 128 + S + 8) * Hq < 2^24.
  * ws: chipmunk_attn_paged_workspace_bytes() (0: ws may be NULL; also 0 on bad arguments) of the same sizes, contents undefined afterwards,
- * not to be shared by calls that may overlap. */
+ * not to be shared by calls that may overlap.  Its room goes by S * max_q and is bounded: a long chunk beside single tokens of other sequences is
+ * walked in fewer parts than alone, or in none, and is quicker in a call of its own. */
 size_t chipmunk_attn_paged_workspace_bytes(int S, int Hq, int Hk, int E, int max_q, int max_k, int window, int sinks);
 int32_t chipmunk_attn_paged(const uint16_t* q, int64_t q_token_stride, int64_t q_head_stride, const chipmunk_pages* pages, const int32_t* table,
                             int64_t table_stride, int table_pages, uint16_t* out, int64_t out_token_stride, int64_t out_head_stride, const int32_t* cu_q,

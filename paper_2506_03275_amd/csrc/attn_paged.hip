@@ -1,6 +1,7 @@
 // Attention of new tokens over sequences in pages (chipmunk_pages): one token of a sequence, a few or a chunk of them, causal or not, every key or
 // a sliding window and the sequence's first keys; pages of 16 bits, or e4m3 whose rows are brought to the element type on their way to LDS, so that
-// a call over codes gives bit by bit what it gives over the elements that they stand for.
+// a form gives over codes bit by bit what it gives over the elements that they stand for (the prices of either may choose another form, whose sums
+// are rounded elsewhere: 1 query over 900 keys, 32 heads over 8).
 //
 // The kernels are those of attention over packed sequences (attn_packed.hip, attn_tiles.h) with other keys: a workgroup walks a row of "numbered" keys,
 // those that some of its rows may see, those first that all of them may (an online softmax has no order).  Where groups of 16 numbered keys
@@ -173,8 +174,8 @@ __device__ __forceinline__ void add_special_values(RowState<T, E, NQB>& st, cons
 
 // Few queries over many keys, as attn_packed_few_kernel: a workgroup owns one key head of one sequence and walks part_keys of its numbered keys for
 // block_rows rows of the head; its waves take the tiles of 32 keys in turn and meet at the end.  Bound by the pages' bytes: 16 tokens over 1 to 32 011 keys
-// each, 32 heads over 8 x 128, e4m3: 93 us (4.7 TB/s), where a launch's round trips (lengths, table, first tiles) and its parts' ends are some 10 of them;
-// joining takes 6 us.
+// each, 32 heads over 8 x 128, e4m3: 98 us (4.4 TB/s), where a launch's round trips (lengths, table, first tiles) and its parts' ends are some 10 of them;
+// joining takes 6 us.  (64 rows of codes at E = 128 keep 22 registers in scratch memory: 64 queries over 2000 keys 26 us, of elements, in whole walks, 16.6.)
 template <class T, int E, int NQB, bool CODES>
 __global__ __launch_bounds__(256, NQB == 4 ? 1 : NQB == 1 && CODES ? 3 : 2) void attn_paged_few_kernel(PagedParams p) {
     typedef typename T::x8 x8;
@@ -351,7 +352,8 @@ __device__ __forceinline__ float* partial_stats(const PagedParams& p) { return p
 // two tiles of 32.  Elements go from the pages to LDS by asynchronous loads, double buffered by step; codes are in registers a step before, and go to LDS
 // as elements while the step before theirs is computed.  Of few rows over many keys a workgroup walks part_keys of them (gridDim.y parts), and
 // attn_paged_join_rows_kernel joins the parts.  Bound by the matrix pipes and the softmax beside them, as attn_packed_rows_kernel: chunks of 33 to 1024
-// tokens over 1000 to 16 384 keys, 32 heads over 8 x 128: 386 to 408 us, the matrix pipes busy 51 % and the vector units 45 % of the time at 2.0 GHz.
+// tokens over 1000 to 16 384 keys, 32 heads over 8 x 128: 386 to 408 us a pass; in passes of 437 us under the counters the matrix pipes are busy 51 % and
+// the vector units 45 % of the time at 2.04 GHz.
 template <class T, int E, int NQB, bool CODES>
 __global__ __launch_bounds__(256, E == 64 ? 3 : 2) void attn_paged_rows_kernel(PagedParams p) {
     typedef typename T::x8 x8;
@@ -726,6 +728,9 @@ constexpr RowPartsPrice kRowPartsPrices[2][2] = {{{{{64, 1.96f, 0.9f, 0.295f}, {
                                                  {{{{64, 2.4f, 0.84f, 0.33f}, {128, 2.f, 1.3f, 0.242f}}, 0.089f, 2.8f, 0.26f},          // codes
                                                   {{{64, 5.9f, 0.84f, 0.61f}, {128, 3.9f, 1.49f, 0.387f}}, 0.63f, 4.8f, 0.165f}}};
 constexpr int64_t kMostRowPartBytes = 64 << 20;
+// (By S * max_q, whether or not the sequences have so many: the workspace is asked for without the number of queries that there are, and a part's rows are
+// found by their sequence.  So a chunk beside other sequences' single tokens has room for fewer parts than alone, or for none: 512 queries over 32 768
+// keys 296 us, with one token over as many beside it 323, with three 784, where the three by themselves take 86.)
 constexpr int kLeastRowPart = 512, kMostRowParts = 16;   // keys; parts
 static int64_t row_part_bytes(int S, int Hq, int E, int max_q) { return (int64_t)S * Hq * max_q * (E + 2) * (int64_t)sizeof(float); }
 // The parts that there may be, by the room for their sums, by the keys and by the CUs, of any number of queries within the limits.

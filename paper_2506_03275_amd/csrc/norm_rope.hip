@@ -3,8 +3,8 @@
 // and the gradient: with g = turn^-1(grad), c = mean_e(g_e w_e n_e),
 //     dx = r (g w - n c),       dw_e = sum over rows of g_e n_e.
 //
-// Bound: memory; 4 E bytes per row of a head, the gradient 6 E.  18 000 tokens of 80 heads x 128: 130 us (5.7 TB/s), the gradient 214 (5.2 TB/s);
-// 4608 tokens of 48 heads 20.3 us (5.6 TB/s); 8 tokens of 40 heads 3.7.
+// Bound: memory; 4 E bytes per row of a head, the gradient 6 E.  18 000 tokens of 80 heads x 128: 130 us (5.7 TB/s), the gradient 220 (5.0 TB/s);
+// 4608 tokens of 48 heads 20.2 us (5.6 TB/s); 8 tokens of 40 heads 3.7 to 4.0.
 #include "rope.h"
 
 #include <algorithm>
